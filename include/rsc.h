@@ -4,7 +4,9 @@
  * top-k column-row approximation (score pairs, keep the top k, slice the
  * kept columns out of the CSR matrix, cache the slice, run SpMM on it);
  * also the unbiased randomized column-row sampler, the MEAN-aggregator
- * operand, the layer-wise budget allocation and a CSR validity check.
+ * operand, the layer-wise budget allocation and a CSR validity check; and the
+ * update phase of a training step (a layer's product with its epilogue, the
+ * class loss, the AdamW step).
  *
  * Paper: Liu et al., "RSC: Accelerate Graph Neural Networks Training via
  * Randomized Sparse Computations", ICML 2023 (arXiv 2210.10737).
@@ -20,7 +22,8 @@
  *     rsc_cache_get are borrowed from the cache.
  *   - Dense matrices are row-major fp32 with a leading dimension (in floats)
  *     ld >= d, ld % 4 == 0, and a 16-byte-aligned base pointer. Columns
- *     d .. ld-1 of an output are never written.
+ *     d .. ld-1 of an output are never written. (The update phase's calls
+ *     take 16-bit types too; see there.)
  *   - CSR matrices: int32 row pointers and column indices, fp32 values,
  *     nnz < 2^31, columns strictly increasing within each row.
  *   - No C++ exception crosses this interface. Asynchronous device faults
@@ -497,6 +500,146 @@ rsc_status_t rsc_greedy_allocate_profiles(int32_t L, int32_t n, int64_t nnz, int
                                           double fro_a2, const double *fro_b2_host, int32_t C_num,
                                           int32_t C_den, int32_t *k_out_host,
                                           int64_t *budget_out_host);
+
+/* ------------------------------------------------ the update phase --- */
+/* What a training step does between and after the aggregations: the product
+ * with a layer's weights and its epilogue, the class loss, the optimizer
+ * step. Operands are fp32, bf16 or fp16; every sum is held in fp32 or wider
+ * and each result is rounded once to its type.
+ *   - Matrices are row-major with a leading dimension ld (in values); a row
+ *     is a whole number of 16 bytes (ld * size % 16 == 0) of at most 4 MiB
+ *     and the base pointer is 16-byte aligned. What lies between a row's last
+ *     value and the next row is not used and, in outputs, not written.
+ *   - Vectors (bias, its gradient) are contiguous, of the operands' type or,
+ *     with bias_dtype RSC_F32, fp32.
+ *   - Workspaces are 256-byte aligned and private to the call until it
+ *     completes on `stream`. All calls only launch kernels: they can be
+ *     captured into a HIP graph, whose replays read and write the same
+ *     buffers and hold the scalar arguments of the capture. Results are
+ *     bitwise reproducible.
+ *   - Sizes must keep the number of 32 x 64 tiles of every product below 2^30
+ *     (RSC_ERR_UNSUPPORTED). */
+typedef enum { RSC_F32 = 0, RSC_BF16 = 1, RSC_F16 = 2 } rsc_dtype_t;
+typedef enum { RSC_ACT_NONE = 0, RSC_ACT_RELU = 1, RSC_ACT_GELU = 2, RSC_ACT_SILU = 3 } rsc_act_t;
+
+/* Y = act(Z), Z = alpha X W + bias + beta R.
+ *   X: n x k. R, Y: n x m. W: k x m, stored as k rows of m values
+ *   (w_out_major = 0, ldw >= m) or as m rows of k values (w_out_major = 1,
+ *   ldw >= k). n >= 0, k >= 1, m >= 1.
+ *   act: none, max(z, 0), z Phi(z) (the exact GELU), z / (1 + exp(-z)). */
+typedef struct {
+    int32_t dtype; /* rsc_dtype_t of X, W, R, Y */
+    int32_t act;   /* rsc_act_t */
+    int32_t n, k, m;
+    int32_t w_out_major;
+    float alpha, beta;
+} rsc_linear_t;
+
+/* rsc_linear: bias, R and pre may be NULL; pre (n x m) receives Z, which the
+ * backward pass of GELU and SiLU needs. Y may be R (in place) but must not
+ * overlap X or W. fp32 products are formed from three bf16 parts a value
+ * (24 bits in all, six partial products): finite operands of magnitude below
+ * 3.3e38 give fp32 accuracy; an infinite operand gives NaN.
+ * Workspace: 0 bytes unless the sums over k are split over blocks. */
+size_t rsc_linear_workspace_bytes(const rsc_linear_t *p);
+rsc_status_t rsc_linear(const rsc_linear_t *p, const void *X, int64_t ldx, const void *W, int64_t ldw,
+                        const void *bias, int32_t bias_dtype, const void *R, int64_t ldr, void *Y, int64_t ldy,
+                        void *pre, int64_t ldpre, void *ws, size_t ws_bytes, hipStream_t stream);
+/* Gradients for dY: dZ = dY act'(Z), dX = alpha dZ W^T, dW = alpha X^T dZ
+ * (stored as W is), dbias = sum over rows of dZ, dR = beta dZ; each output
+ * may be NULL (X may be NULL without dW, W without dX). dZ is held in the operands' type. saved: Y for ReLU (its slope is 1
+ * where Y > 0), pre for GELU and SiLU, unused (NULL) without an activation.
+ * n = 0 gives zero dW and dbias. The workspace holds dZ (with an activation),
+ * partial sums of dbias and of split products; its size covers the outputs
+ * named by the flags. */
+size_t rsc_linear_backward_workspace_bytes(const rsc_linear_t *p, int32_t with_dx, int32_t with_dw,
+                                           int32_t with_dbias);
+rsc_status_t rsc_linear_backward(const rsc_linear_t *p, const void *dY, int64_t lddy, const void *saved,
+                                 int64_t ldsaved, const void *X, int64_t ldx, const void *W, int64_t ldw, void *dX,
+                                 int64_t lddx, void *dW, int64_t lddw, void *dbias, int32_t bias_dtype, void *dR,
+                                 int64_t lddr, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Softmax cross entropy of the logits L = X W + bias (n x v) against one
+ * class a row: loss_r = log sum_j exp(L_rj) - L_r,t(r). The logits are not
+ * kept: the forward pass forms them tile by tile, the backward pass again in
+ * pieces of the classes.
+ *   targets: n values, int64 or int32 (targets_i32). Rows whose target is
+ *   ignore_index are left out: loss 0, gradients 0 (their X rows must still be
+ *   finite: they enter dW times 0). Any other target outside 0 .. v-1 gives
+ *   NaN.
+ *   reduction: 0 = loss per row (n values), 1 = sum, 2 = mean over the rows
+ *   not left out (0 if there is none). */
+typedef struct {
+    int32_t dtype; /* rsc_dtype_t of X, W */
+    int32_t n, k, v;
+    int32_t w_out_major;
+    int32_t reduction;
+    int32_t targets_i32;
+    int32_t bias_dtype;
+    int64_t ignore_index;
+} rsc_xent_t;
+
+/* rsc_xent: loss (fp32; 1 value, or n with reduction 0), lse (n values: log
+ * sum exp of each row's logits) and count (1 value: what the loss was divided
+ * by; unused with reduction 0) are outputs that the backward pass reads. */
+size_t rsc_xent_workspace_bytes(const rsc_xent_t *p);
+rsc_status_t rsc_xent(const rsc_xent_t *p, const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias,
+                      const void *targets, float *loss, float *lse, float *count, void *ws, size_t ws_bytes,
+                      hipStream_t stream);
+/* Gradients for dloss (device, fp32; 1 value, or n with reduction 0): dX (n x
+ * k), dW (stored as W is) and dbias, each may be NULL. The workspace holds
+ * one piece of the logits' gradient (256 MiB, or n x 2,048 values where that
+ * is more) and, with more than one piece, dX in fp32. */
+size_t rsc_xent_backward_workspace_bytes(const rsc_xent_t *p, int32_t with_dx, int32_t with_dw);
+rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const void *X, int64_t ldx, const void *W,
+                               int64_t ldw, const void *bias, const void *targets, const float *lse,
+                               const float *count, void *dX, int64_t lddx, void *dW, int64_t lddw, void *dbias,
+                               void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* One AdamW step over `count` tensors:
+ *   t = ++*step;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay)
+ *       - (m lr / (1 - beta1^t)) / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, every operation rounded by itself. Tensors are contiguous, n
+ * values each (0 allowed), and must not overlap one another.
+ *   param, grad: `dtype`. master (nullable): fp32 values that the step is
+ *   applied to; param then receives their rounding.
+ *   state_bits 32: exp_avg, exp_avg_sq are fp32 (m, v).
+ *   state_bits 8: exp_avg is int8, exp_avg_sq uint8, with one fp32 scale per
+ *   256 elements (ceil(n / 256) each): m = s q |q| / 127^2, sqrt(v) = s
+ *   (q / 255)^2, s the block's largest |m| or sqrt(v). Codes are rounded up
+ *   with the probability of their remainder, by 24-bit draws from output
+ *   number t 2^40 + base + i + 1 of SplitMix64 seeded with `seed` (base: the
+ *   preceding tensors' sizes, each rounded up to 256); sqrt(v) > 0 keeps a
+ *   code of at least 1. A NaN gradient makes its block NaN.
+ *   step: device, int64; incremented by the call, so a captured call advances
+ *   with each replay. lr and the other options are those of the capture.
+ * The descriptors are read on the host before the call returns. Workspace:
+ * rsc_adamw_workspace_bytes(). */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *exp_avg, *exp_avg_sq;
+    float *master;
+    float *exp_avg_scale, *exp_avg_sq_scale;
+    int64_t n;
+} rsc_adamw_tensor_t;
+typedef struct {
+    int32_t dtype;      /* rsc_dtype_t of param and grad */
+    int32_t state_bits; /* 32 or 8 */
+    double lr, beta1, beta2, eps, weight_decay;
+    uint64_t seed;
+} rsc_adamw_t;
+size_t rsc_adamw_workspace_bytes(void);
+rsc_status_t rsc_adamw_step(const rsc_adamw_t *p, const rsc_adamw_tensor_t *tensors_host, int32_t count,
+                            int64_t *step, void *ws, size_t ws_bytes, hipStream_t stream);
+/* The values that 8-bit moments stand for: exp_avg_out = m, exp_avg_sq_out =
+ * v (fp32, n values of each tensor; `param`, `grad` and `master` of the
+ * descriptors are not used). The output arrays are host arrays of `count` device
+ * pointers. */
+rsc_status_t rsc_adamw_moments(const rsc_adamw_tensor_t *tensors_host, int32_t count,
+                               float *const *exp_avg_out_host, float *const *exp_avg_sq_out_host,
+                               hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -22,6 +22,14 @@ Typical use (A_hat symmetric, so it serves as its own transpose):
     G_back = cache.spmm_sampled(G)                       # sampled backward
 
 `gcn.GCN` wires these into a training step with the layer-wise allocation.
+
+The update phase between two aggregations (fp32, bf16, fp16; differentiable):
+
+    H = linear(P, W, b, residual=H, act="relu")          # act(P W + b + H)
+    loss = linear_cross_entropy(H, W_out, classes)       # no n x classes logits in memory
+    opt = AdamW(params, state_bits=8)                    # one launch over all tensors
+
+`gcn.GCNClassifier` is built from these and the aggregation.
 """
 from __future__ import annotations
 
@@ -54,6 +62,9 @@ EXPORTED = [
     "rsc_k_from_fraction", "rsc_greedy_allocate",
     "rsc_greedy_profile_workspace_bytes", "rsc_greedy_blocks", "rsc_greedy_profile",
     "rsc_greedy_allocate_profiles",
+    "rsc_linear_workspace_bytes", "rsc_linear", "rsc_linear_backward_workspace_bytes", "rsc_linear_backward",
+    "rsc_xent_workspace_bytes", "rsc_xent", "rsc_xent_backward_workspace_bytes", "rsc_xent_backward",
+    "rsc_adamw_workspace_bytes", "rsc_adamw_step", "rsc_adamw_moments",
 ]
 
 
@@ -91,6 +102,24 @@ def _torch_allocator() -> Allocator:
 class CsrStruct(ctypes.Structure):
     _fields_ = [("n_rows", ctypes.c_int32), ("n_cols", ctypes.c_int32), ("nnz", ctypes.c_int64),
                 ("rowptr", ctypes.c_void_p), ("col", ctypes.c_void_p), ("val", ctypes.c_void_p)]
+
+
+class LinearStruct(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("m", ctypes.c_int32), ("w_out_major", ctypes.c_int32), ("alpha", ctypes.c_float),
+                ("beta", ctypes.c_float)]
+
+
+class XentStruct(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32), ("v", ctypes.c_int32),
+                ("w_out_major", ctypes.c_int32), ("reduction", ctypes.c_int32), ("targets_i32", ctypes.c_int32),
+                ("bias_dtype", ctypes.c_int32), ("ignore_index", ctypes.c_int64)]
+
+
+class AdamwStruct(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("lr", ctypes.c_double),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("seed", ctypes.c_uint64)]
 
 
 _lib = None
@@ -155,6 +184,21 @@ def lib():
             "rsc_greedy_profile": ([vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp], ctypes.c_int),
             "rsc_greedy_allocate_profiles": ([i32, i32, i64, i32, i32, vp, vp, vp, ctypes.c_double, vp,
                                               i32, i32, vp, vp], ctypes.c_int),
+            "rsc_linear_workspace_bytes": ([ctypes.POINTER(LinearStruct)], sz),
+            "rsc_linear": ([ctypes.POINTER(LinearStruct), vp, i64, vp, i64, vp, i32, vp, i64, vp, i64, vp, i64, vp,
+                            sz, vp], ctypes.c_int),
+            "rsc_linear_backward_workspace_bytes": ([ctypes.POINTER(LinearStruct), i32, i32, i32], sz),
+            "rsc_linear_backward": ([ctypes.POINTER(LinearStruct), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp,
+                                     i64, vp, i32, vp, i64, vp, sz, vp], ctypes.c_int),
+            "rsc_xent_workspace_bytes": ([ctypes.POINTER(XentStruct)], sz),
+            "rsc_xent": ([ctypes.POINTER(XentStruct), vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp],
+                         ctypes.c_int),
+            "rsc_xent_backward_workspace_bytes": ([ctypes.POINTER(XentStruct), i32, i32], sz),
+            "rsc_xent_backward": ([ctypes.POINTER(XentStruct), vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64,
+                                   vp, vp, sz, vp], ctypes.c_int),
+            "rsc_adamw_workspace_bytes": ([], sz),
+            "rsc_adamw_step": ([ctypes.POINTER(AdamwStruct), vp, i32, vp, vp, sz, vp], ctypes.c_int),
+            "rsc_adamw_moments": ([vp, i32, vp, vp, vp], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -660,3 +704,7 @@ def greedy_allocate_profiles(masses, counts, n: int, nnz: int, d, fro_a2: float,
                                               float(fro_a2), fb.ctypes.data, C[0], C[1],
                                               k_out.ctypes.data, ctypes.byref(bud)))
     return [int(x) for x in k_out], int(bud.value)
+
+
+# ---------------------------------------------------------------- update phase
+from .update import (AdamW, adamw_moments, adamw_step, linear, linear_cross_entropy)  # noqa: E402,F401

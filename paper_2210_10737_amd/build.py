@@ -15,7 +15,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "librsc.so")
-SOURCES = ["spmm.hip", "scores.hip", "topk.hip", "slice.hip", "greedy.hip", "mean.hip", "sample.hip", "validate.hip", "hub.hip", "probe.hip", "api.hip"]
+SOURCES = ["spmm.hip", "scores.hip", "topk.hip", "slice.hip", "greedy.hip", "mean.hip", "sample.hip", "validate.hip", "hub.hip", "probe.hip", "api.hip",
+           "gemm_f32_rr.hip", "gemm_f32_rc.hip", "gemm_f32_cc.hip", "gemm_bf16_rr.hip", "gemm_bf16_rc.hip",
+           "gemm_bf16_cc.hip", "gemm_f16_rr.hip", "gemm_f16_rc.hip", "gemm_f16_cc.hip", "linear.hip", "loss.hip",
+           "adamw.hip", "api_update.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -1,0 +1,329 @@
+// One AdamW step over many tensors at once, the moments in 32 bits or in 8.
+//
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
+//   p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// 8 bits: blocks of 256 elements with their largest value s. The first moment
+// is s (q / 127) |q / 127|, q in -127 .. 127; the second is held as its root,
+// s (q / 255)^2, q in 0 .. 255, so that both resolve values far below the
+// block's largest (6e-5 and 1.5e-5 of it). A step changes v by a thousandth,
+// less than a code: codes are rounded up or down at random in proportion
+// (SplitMix64 of seed, step and element), so that the changes add up. A root
+// above zero keeps a code of at least 1, which bounds m / sqrt(v).
+//
+// Bound by memory: every value is read and written once, 256 threads take
+// 4,096 consecutive elements of a tensor, a wave 256 at a time (one block of
+// codes: its largest value is a reduction over the wave). All tensors of a
+// launch are in its arguments, so that a captured launch holds them.
+//
+// Each operation rounds by itself (no contraction): the step is defined to the
+// bit, and codes next to a border do not hang on the compiler.
+#include "rsc_internal.h"
+#include "adamw.h"
+
+namespace rsc {
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int8_t v4c __attribute__((ext_vector_type(4)));
+typedef uint8_t v4u __attribute__((ext_vector_type(4)));
+
+struct AdamwTensor : rsc_adamw_tensor_t {
+    int32_t aligned;  // every pointer to 16 bytes
+};
+
+constexpr int kTensors = 44;  // of a launch: their descriptors fit 4 KB of arguments
+constexpr int kChunk = 4096;  // elements a thread block
+
+struct Batch {
+    AdamwTensor t[kTensors];
+    uint64_t first[kTensors];      // number of the tensor's first random word
+    int32_t end[kTensors];         // thread blocks up to and with the tensor
+    int32_t count;
+};
+static_assert(sizeof(Batch) + sizeof(AdamwRates) + 64 <= 4096, "kernel arguments");
+
+// what depends on the step's number
+struct Now {
+    float rate, unbias;
+    int64_t step;
+};
+
+// step += 1, and the bias corrections for it
+__global__ void begin_kernel(int64_t *step, AdamwRates a, Now *now) {
+    const int64_t t = *step + 1;
+    *step = t;
+    now->step = t;
+    now->rate = (float)(a.lr / (1.0 - pow(a.beta1, (double)t)));
+    now->unbias = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)t)));
+}
+
+__device__ __forceinline__ uint64_t mix(uint64_t seed, uint64_t number) {
+    uint64_t z = seed + number * 0x9E3779B97F4A7C15ull;
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
+
+// the largest of the wave's non-negative values; as integers, so that a NaN is
+// above all and is kept
+__device__ __forceinline__ float wave_max(float x) {
+    uint32_t v = __float_as_uint(x);
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) v = max(v, (uint32_t)__shfl_xor((int)v, d));
+    return __uint_as_float(v);
+}
+
+__device__ __forceinline__ float decode(float code, float by) {
+#pragma clang fp contract(off)
+    const float w = code * by;
+    return w * fabsf(w);
+}
+
+__device__ __forceinline__ float encode(float x, float scale, float levels, uint32_t bits) {
+#pragma clang fp contract(off)
+    const float share = x / (scale > 0.f ? scale : 1.f);
+    const float u = (float)bits * 0x1p-24f;
+    return fminf(floorf(sqrtf(share) * levels + u), levels);
+}
+
+template <typename T, int COUNT>
+__device__ __forceinline__ void get4(const T *p, int n, bool vec, T (&v)[COUNT]) {
+    typedef T v4 __attribute__((ext_vector_type(4)));
+    if (vec) {
+        const v4 x = *(const v4 *)p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : (T)0;
+    }
+}
+template <typename T, int COUNT>
+__device__ __forceinline__ void put4(T *p, int n, bool vec, const T (&v)[COUNT]) {
+    typedef T v4 __attribute__((ext_vector_type(4)));
+    if (vec) {
+        v4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = v[i];
+        *(v4 *)p = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = v[i];
+    }
+}
+
+template <typename T, bool CODES>
+__global__ __launch_bounds__(256) void step_kernel(Batch b, AdamwRates a, const Now *now) {
+#pragma clang fp contract(off)
+    // the block's tensor: the first one whose last block is not before it
+    int lo = 0, hi = b.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if ((int)blockIdx.x < b.end[mid]) hi = mid;
+        else lo = mid + 1;
+    }
+    const AdamwTensor t = b.t[lo];
+    const int64_t chunk = (int64_t)blockIdx.x - (lo ? b.end[lo - 1] : 0);
+    const int64_t from = chunk * kChunk + (int64_t)(threadIdx.x >> 6) * 256 + (threadIdx.x & 63) * 4;
+    const float rate = now->rate, unbias = now->unbias;
+    const uint64_t base = (uint64_t)now->step * (1ull << 40) + b.first[lo] + 1;
+#pragma unroll
+    for (int k = 0; k < kChunk / 1024; ++k) {
+        const int64_t at = from + k * 1024;
+        if (at - (threadIdx.x & 63) * 4 >= t.n) break;  // the whole wave is past the end
+        const int n = (int)min((int64_t)4, t.n - at);   // may be 0 or less at the end
+        const bool vec = t.aligned && n == 4;
+        float p[4], g[4], m[4], r[4], v[4];
+        {
+            T x[4];
+            get4((const T *)t.grad + at, n, vec, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[i] = (float)x[i];
+        }
+        if (t.master) {
+            get4(t.master + at, n, vec, p);
+        } else {
+            T x[4];
+            get4((const T *)t.param + at, n, vec, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = (float)x[i];
+        }
+        const int64_t block = at >> 8;
+        if (CODES) {
+            int8_t q[4];
+            uint8_t c[4];
+            get4((const int8_t *)t.exp_avg + at, n, vec, q);
+            get4((const uint8_t *)t.exp_avg_sq + at, n, vec, c);
+            const float qs = t.exp_avg_scale[block], rs = t.exp_avg_sq_scale[block];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                m[i] = decode((float)q[i], (float)(1.0 / 127)) * qs;
+                const float root = decode((float)c[i], (float)(1.0 / 255)) * rs;
+                v[i] = root * root;
+            }
+        } else {
+            get4((const float *)t.exp_avg + at, n, vec, m);
+            get4((const float *)t.exp_avg_sq + at, n, vec, v);
+        }
+        float m_top = 0.f, r_top = 0.f;
+        uint32_t m_bits = 0, r_bits = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[i] = m[i] * a.b1 + g[i] * a.c1;
+            v[i] = v[i] * a.b2 + (g[i] * a.c2) * g[i];
+            r[i] = sqrtf(v[i]);
+            p[i] = p[i] * a.keep - (m[i] * rate) / (r[i] * unbias + a.eps);
+            if (CODES && i < n) {
+                m_bits = max(m_bits, __float_as_uint(fabsf(m[i])));
+                r_bits = max(r_bits, __float_as_uint(r[i]) & 0x7fffffffu);
+            }
+        }
+        if (t.master) put4(t.master + at, n, vec, p);
+        {
+            T x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = (T)p[i];
+            put4((T *)t.param + at, n, vec, x);
+        }
+        if (CODES) {
+            m_top = wave_max(__uint_as_float(m_bits));
+            r_top = wave_max(__uint_as_float(r_bits));
+            int8_t q[4];
+            uint8_t c[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t z = mix(a.seed, base + (uint64_t)(at + i));
+                const float qm = encode(fabsf(m[i]), m_top, 127.f, (uint32_t)(z & 0xffffffu));
+                q[i] = (int8_t)(m[i] < 0.f ? -qm : qm);
+                const float qr = encode(r[i], r_top, 255.f, (uint32_t)((z >> 24) & 0xffffffu));
+                c[i] = (uint8_t)(r[i] > 0.f ? fmaxf(qr, 1.f) : qr);
+            }
+            put4((int8_t *)t.exp_avg + at, n, vec, q);
+            put4((uint8_t *)t.exp_avg_sq + at, n, vec, c);
+            if ((threadIdx.x & 63) == 0) {
+                t.exp_avg_scale[block] = m_top;
+                t.exp_avg_sq_scale[block] = r_top;
+            }
+        } else {
+            put4((float *)t.exp_avg + at, n, vec, m);
+            put4((float *)t.exp_avg_sq + at, n, vec, v);
+        }
+    }
+}
+
+// the values that 8-bit moments stand for
+__global__ __launch_bounds__(256) void moments_kernel(Batch b) {
+#pragma clang fp contract(off)
+    int lo = 0, hi = b.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if ((int)blockIdx.x < b.end[mid]) hi = mid;
+        else lo = mid + 1;
+    }
+    const AdamwTensor t = b.t[lo];
+    const int64_t chunk = (int64_t)blockIdx.x - (lo ? b.end[lo - 1] : 0);
+    const int64_t from = chunk * kChunk + threadIdx.x * 4;
+#pragma unroll
+    for (int k = 0; k < kChunk / 1024; ++k) {
+        const int64_t at = from + k * 1024;
+        if (at >= t.n) break;
+        const int n = (int)min((int64_t)4, t.n - at);
+        const bool vec = t.aligned && n == 4;
+        int8_t q[4];
+        uint8_t c[4];
+        get4((const int8_t *)t.exp_avg + at, n, vec, q);
+        get4((const uint8_t *)t.exp_avg_sq + at, n, vec, c);
+        const float qs = t.exp_avg_scale[at >> 8], rs = t.exp_avg_sq_scale[at >> 8];
+        float m[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[i] = decode((float)q[i], (float)(1.0 / 127)) * qs;
+            const float root = decode((float)c[i], (float)(1.0 / 255)) * rs;
+            v[i] = root * root;
+        }
+        put4(t.master + at, n, vec, m);
+        put4((float *)t.param + at, n, vec, v);
+    }
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// f(batch, thread blocks) for the tensors in groups that fit a launch
+template <typename F>
+hipError_t in_batches(const rsc_adamw_tensor_t *t, int32_t count, F f) {
+    Batch b;
+    b.count = 0;
+    int64_t blocks = 0;
+    uint64_t first = 0;
+    hipError_t e = hipSuccess;
+    auto flush = [&] {
+        if (b.count && e == hipSuccess) e = f(b, (unsigned)blocks);
+        b.count = 0;
+        blocks = 0;
+    };
+    for (int32_t i = 0; i < count; ++i) {
+        const rsc_adamw_tensor_t &x = t[i];
+        if (x.n == 0) continue;
+        const int64_t need = ceil_div(x.n, kChunk);
+        if (b.count == kTensors || blocks + need > (int64_t(1) << 30)) flush();
+        blocks += need;
+        static_cast<rsc_adamw_tensor_t &>(b.t[b.count]) = x;
+        // 16-bit parameters and codes move by 8 and 4 bytes, which 16 covers
+        b.t[b.count].aligned = aligned16(x.param) && aligned16(x.grad) && aligned16(x.exp_avg) &&
+                               aligned16(x.exp_avg_sq) && aligned16(x.master);
+        b.first[b.count] = first;
+        b.end[b.count] = (int32_t)blocks;
+        ++b.count;
+        first += (uint64_t)ceil_div(x.n, 256) * 256;
+    }
+    flush();
+    return e;
+}
+
+}  // namespace
+
+size_t adamw_ws_bytes() { return 256; }
+static_assert(sizeof(Now) <= 256, "workspace");
+
+hipError_t adamw_launch(int32_t dtype, int32_t codes, const rsc_adamw_tensor_t *t, int32_t count, const AdamwRates &a,
+                        int64_t *step, void *ws, hipStream_t stream) {
+    Now *now = (Now *)ws;
+    begin_kernel<<<1, 1, 0, stream>>>(step, a, now);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return in_batches(t, count, [&](const Batch &b, unsigned blocks) {
+        if (dtype == 0 && codes) step_kernel<float, true><<<blocks, 256, 0, stream>>>(b, a, now);
+        else if (dtype == 0) step_kernel<float, false><<<blocks, 256, 0, stream>>>(b, a, now);
+        else if (dtype == 1 && codes) step_kernel<__bf16, true><<<blocks, 256, 0, stream>>>(b, a, now);
+        else if (dtype == 1) step_kernel<__bf16, false><<<blocks, 256, 0, stream>>>(b, a, now);
+        else if (codes) step_kernel<_Float16, true><<<blocks, 256, 0, stream>>>(b, a, now);
+        else step_kernel<_Float16, false><<<blocks, 256, 0, stream>>>(b, a, now);
+        return hipGetLastError();
+    });
+}
+
+hipError_t adamw_moments_launch(const rsc_adamw_tensor_t *t, int32_t count, float *const *m, float *const *v,
+                                hipStream_t stream) {
+    for (int32_t i = 0; i < count;) {
+        // the outputs stand where the parameters do in a step
+        rsc_adamw_tensor_t some[kTensors];
+        int32_t have = 0;
+        for (; i < count && have < kTensors; ++i) {
+            some[have] = t[i];
+            some[have].param = v[i];
+            some[have].grad = nullptr;
+            some[have].master = m[i];
+            ++have;
+        }
+        const hipError_t e = in_batches(some, have, [&](const Batch &b, unsigned blocks) {
+            moments_kernel<<<blocks, 256, 0, stream>>>(b);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace rsc

@@ -1,0 +1,252 @@
+"""The class loss and its gradients against the formula in 64 bits.
+
+Tolerances: a logit is off by at most 2 (k + 8) 2^-24 of its sum of magnitudes
+(as in the layer's tests), `z` at most over a row; log sum exp by z and by the
+relative error of a sum of positive terms: at most 600 additions in a chain
+(16 within a lane's tile columns, 4 waves, the tiles) and an exponential
+within 2^-20 of its value (|arguments| up to 16 log2 e, rounded to 24 bits), so 2^-14 in
+all with room; the gradient of a logit is off by its share of both and, held
+in the operands' type, by half a step."""
+import math
+
+import pytest
+import torch
+
+import paper_2210_10737_amd as rsc
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+# the last two: several pieces of the vocabulary in the backward pass
+SIZES = [(1, 1, 1), (1, 8, 2), (3, 5, 7), (17, 64, 33), (33, 100, 257), (130, 33, 64), (300, 257, 70), (64, 1000, 41),
+         (257, 64, 1500), (1, 512, 5000), (4000, 24, 300), (2, 64, 70001)]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu(gpu):
+    yield
+
+
+def half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def sums(k):
+    return 2 * (k + 8) * 2.0 ** -24
+
+
+def rand(shape, dtype, g, scale=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def close(got, want, bound, what):
+    got = got.double()
+    assert got.shape == want.shape, what
+    bad = (got - want).abs() - bound
+    assert bool((bad <= 0).all()), (what, float(bad.max()), float(want.abs().max()))
+
+
+def inputs(n, k, v, dtype, out_major, valid, seed, ignore=-100, i32=False):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = rand((n, k), dtype, g)
+    w = rand((v, k), dtype, g, 2 / math.sqrt(k)).t() if out_major else rand((k, v), dtype, g, 2 / math.sqrt(k))
+    b = rand((v,), dtype, g)
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    t[torch.rand(n, generator=g, device="cuda") >= valid] = ignore
+    return x, w, b, t.int() if i32 else t
+
+
+def reference(x, w, b, t, ignore, reduction, up):
+    """(rows' losses, their bound, gradients with their bounds) in 64 bits."""
+    x, w = x.detach().double(), w.detach().double()
+    dtype_half = 0
+    k = x.shape[1]
+    z, mag = x @ w, x.abs() @ w.abs()
+    if b is not None:
+        z, mag = z + b.detach().double(), mag + b.detach().double().abs()
+    keep = t != ignore
+    t = torch.where(keep, t.long(), torch.zeros_like(t.long()))
+    lse = torch.logsumexp(z, 1)
+    z_off = sums(k) * mag
+    row_off = z_off.amax(1)
+    rows = torch.where(keep, lse - z.gather(1, t[:, None])[:, 0], torch.zeros_like(lse))
+    rows_bound = 2 * row_off + 2.0 ** -14 + 2.0 ** -22 * (lse.abs() + z.abs().amax(1))
+    count = max(1, int(keep.sum()))
+    weight = keep.double() * (up.double() if reduction == "none" else float(up) / (count if reduction == "mean" else 1))
+    p = torch.exp(z - lse[:, None])
+    off = p * (2 * row_off + 2.0 ** -14)[:, None]
+    p.scatter_add_(1, t[:, None], -torch.ones_like(t[:, None], dtype=torch.float64))
+    return rows, rows_bound, weight[:, None] * p, weight.abs()[:, None] * off, weight.abs()[:, None] * p.abs(), count
+
+
+def check(n, k, v, dtype, out_major, bias, valid, reduction="mean", ignore=-100, i32=False, seed=5, up_scale=1.0):
+    x, w, b, t = inputs(n, k, v, dtype, out_major, valid, seed + n + 7 * k + 31 * v, ignore, i32)
+    b = b if bias else None
+    leaves = [a for a in (x, w, b) if a is not None]
+    for a in leaves:
+        a.requires_grad_()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    up = torch.randn(n, generator=g, device="cuda") * up_scale if reduction == "none" else \
+        torch.full((), 1.5 * up_scale, device="cuda")
+    loss = rsc.linear_cross_entropy(x, w, t, b, ignore_index=ignore, reduction=reduction)
+    assert loss.dtype == torch.float32 and tuple(loss.shape) == ((n,) if reduction == "none" else ())
+    rows, rows_bound, grad, grad_off, grad_mag, count = reference(x, w, b, t, ignore, reduction, up)
+    keep = (t != ignore).double()
+    if reduction == "none":
+        close(loss.detach(), rows, rows_bound, ("loss", n, k, v))
+        assert bool((loss.detach()[t == ignore] == 0).all())
+    else:
+        by = count if reduction == "mean" else 1
+        close(loss.detach(), rows.sum() / by, (rows_bound * keep).sum() / by + 2.0 ** -23 * rows.sum() / by + 1e-7,
+              ("loss", n, k, v))
+    with torch.no_grad():
+        assert torch.equal(rsc.linear_cross_entropy(x, w, t, b, ignore_index=ignore, reduction=reduction), loss)
+    got = torch.autograd.grad(loss, leaves, up)
+    # the rounding of G to its type (fp16: half of its smallest step, 2^-25 over 2^10, for small ones)
+    tiny = up.abs().max().double() * 2.0 ** -34 if dtype == torch.float16 else 0.0
+    grad_off = grad_off + (half(dtype) * grad_mag + tiny * (grad_mag > 0)) * (1 if dtype != torch.float32 else 0.5) \
+        + 2.0 ** -22 * grad_mag
+    x6, w6 = x.detach().double(), w.detach().double()
+    small = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps   # a result's own smallest step
+    pieces = 4
+    want, mag = grad @ w6.t(), (grad_mag + grad_off) @ w6.abs().t()
+    off = grad_off @ w6.abs().t() + (sums(v) + pieces * 2.0 ** -23) * mag
+    close(got[0], want, off + half(dtype) * (want.abs() + off) + small, ("dx", n, k, v))
+    assert not got[0][t == ignore].any()
+    want, mag = x6.t() @ grad, x6.abs().t() @ (grad_mag + grad_off)
+    off = x6.abs().t() @ grad_off + (sums(n) + 2.0 ** -23) * mag
+    close(got[1], want, off + half(dtype) * (want.abs() + off) + small, ("dw", n, k, v))
+    if bias:
+        want, off = grad.sum(0), grad_off.sum(0)
+        close(got[2], want, off + half(dtype) * (want.abs() + off) + small, ("db", n, k, v))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("out_major", [False, True])
+@pytest.mark.parametrize("size", SIZES)
+def test_loss_and_gradients(size, out_major, dtype):
+    check(*size, dtype, out_major, bias=True, valid=0.8)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+@pytest.mark.parametrize("valid", [1.0, 0.05, 0.0])
+def test_reductions_and_masks(valid, reduction, dtype):
+    check(70, 48, 300, dtype, True, bias=False, valid=valid, reduction=reduction, i32=True)
+    check(41, 48, 90, dtype, False, bias=True, valid=valid, reduction=reduction, ignore=3)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_small_upstream_gradients(dtype):
+    check(64, 32, 1000, dtype, True, bias=True, valid=0.9, reduction="none", up_scale=2.0 ** -10)
+    check(64, 32, 1000, dtype, True, bias=True, valid=0.9, reduction="none", up_scale=64.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_pieces_of_the_vocabulary(dtype):
+    """More than one piece in the backward pass: 60,000 rows, pieces of 2,048
+    classes or the next multiple of 256."""
+    check(66000, 16, 4500, dtype, True, bias=True, valid=0.9)
+    check(66000, 16, 2300, dtype, False, bias=True, valid=0.9)
+
+
+def test_large_logits_and_masked_classes():
+    """A bias of -inf takes a class out, one of the lowest value nearly so;
+    logits far apart neither overflow nor vanish."""
+    n, k, v = 40, 16, 700
+    x, w, b, t = inputs(n, k, v, torch.float32, True, 1.0, 11)
+    b[100:400] = -float("inf")
+    b[400:410] = torch.finfo(torch.float32).min
+    b[3] = 300.0
+    t.fill_(3)
+    t[0] = 5
+    x.requires_grad_()
+    loss = rsc.linear_cross_entropy(x, w, t, b, reduction="none")
+    z = x.detach().double() @ w.double() + b.double()
+    want = torch.logsumexp(z, 1) - z.gather(1, t[:, None])[:, 0]
+    close(loss.detach(), want, 2.0 ** -14 + 2.0 ** -20 * want.abs(), "loss")
+    gx, = torch.autograd.grad(loss.sum(), x)
+    p = torch.softmax(z, 1)
+    p[torch.arange(n, device="cuda"), t] -= 1
+    close(gx, p @ w.double().t(), torch.full_like(gx, 1e-3, dtype=torch.float64), "dx")
+    t[1] = 200   # the class of a row itself taken out: an infinite loss
+    assert float(rsc.linear_cross_entropy(x.detach(), w, t, b, reduction="none")[1]) == float("inf")
+
+
+def test_targets_out_of_range_show():
+    x, w, b, t = inputs(20, 16, 30, torch.float32, True, 1.0, 2)
+    for bad in (30, -1, 1 << 40):
+        t2 = t.clone()
+        t2[4] = bad
+        rows = rsc.linear_cross_entropy(x, w, t2, b, reduction="none")
+        assert bool(rows.isnan().nonzero()[:, 0].eq(4).all()) and int(rows.isnan().sum()) == 1
+        assert bool(rsc.linear_cross_entropy(x, w, t2, b).isnan())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_no_rows(dtype):
+    x = torch.empty((0, 12), dtype=dtype, device="cuda", requires_grad=True)
+    w = torch.ones((12, 5), dtype=dtype, device="cuda", requires_grad=True)
+    b = torch.ones(5, dtype=dtype, device="cuda", requires_grad=True)
+    t = torch.empty(0, dtype=torch.int64, device="cuda")
+    loss = rsc.linear_cross_entropy(x, w, t, b)
+    assert float(loss) == 0.0
+    gx, gw, gb = torch.autograd.grad(loss, [x, w, b])
+    assert tuple(gx.shape) == (0, 12) and not gw.any() and not gb.any()
+    assert tuple(rsc.linear_cross_entropy(x, w, t, b, reduction="none").shape) == (0,)
+
+
+def test_gradients_against_differences():
+    x, w, b, t = inputs(12, 20, 50, torch.float32, False, 0.8, 3)
+    leaves = [a.requires_grad_() for a in (x, w, b)]
+    grads = torch.autograd.grad(rsc.linear_cross_entropy(x, w, t, b), leaves)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = 2.0 ** -6
+    for i, gr in enumerate(grads):
+        d = rand(tuple(gr.shape), torch.float32, g)
+        d = d / d.norm()
+
+        def at(s):
+            xs, ws, bs = (a.detach() + s * h * d if j == i else a.detach() for j, a in enumerate(leaves))
+            return float(rsc.linear_cross_entropy(xs, ws, t, bs))
+
+        slope, want = (at(1) - at(-1)) / (2 * h), float((gr * d).sum())
+        # third derivatives of a softmax are below 1 in these units, two losses of 5 are rounded at 2^-22
+        assert abs(slope - want) <= h * h + 2 * 2.0 ** -21 / h, (i, slope, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_captured(dtype):
+    x, w, b, t = inputs(150, 64, 500, dtype, True, 0.8, 3)
+    leaves = [a.requires_grad_() for a in (x, w, b)]
+
+    def work():
+        loss = rsc.linear_cross_entropy(x, w, t, b)
+        return [loss.detach(), *torch.autograd.grad(loss, leaves)]
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        work()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = work()
+    for i in range(3):
+        with torch.no_grad():
+            x.mul_(0.9)
+            t[i] = -100
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(held, work()):
+            assert torch.equal(got, want), i
+
+
+def test_refusals():
+    x, w, b, t = inputs(6, 16, 30, torch.float32, True, 1.0, 2)
+    for bad in (dict(targets=t.float()), dict(targets=t[:5]), dict(targets=t.cpu()), dict(reduction="max"),
+                dict(ignore_index=1 << 63), dict(bias=b[:3]), dict(weight=w.half()), dict(x=x.half()), dict(x=x.cpu()),
+                dict(x=x[:, :8])):
+        args = {**dict(x=x, weight=w, targets=t, bias=b), **bad}
+        with pytest.raises(ValueError):
+            rsc.linear_cross_entropy(**args)
