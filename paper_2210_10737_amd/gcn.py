@@ -24,8 +24,10 @@ layer, the AUC of the selection it replaced under the new ranking and the
 overlap of the two selections (section 3.3.1, Fig. 4), computed on the
 device by rsc_cache_staleness from rsc_greedy_profile's ranking.
 
-The dense update phase (MatMul, ReLU, loss, optimizer) uses torch; it is not
-part of the aggregation path.
+GCN's dense update phase (MatMul, ReLU, loss, optimizer) uses torch; it is
+not part of the aggregation path. GCNClassifier's runs on the library: layer
+products with bias, residual and ReLU in their epilogue, softmax cross entropy
+without the logits in memory, and (with rsc.AdamW) the optimizer step.
 """
 from __future__ import annotations
 
@@ -35,7 +37,7 @@ from dataclasses import dataclass, field
 
 import torch
 
-from . import Cache, DeviceCsr, SpmmPlan, _check, _stream, greedy_allocate_profiles, lib
+from . import Cache, DeviceCsr, SpmmPlan, _check, _stream, greedy_allocate_profiles, lib, linear, linear_cross_entropy
 
 
 class _Aggregate(torch.autograd.Function):
@@ -215,6 +217,11 @@ class RscController:
             layer.plan_t.close()
 
 
+def _glorot(fan_in: int, fan_out: int, g: torch.Generator) -> torch.nn.Parameter:
+    a = math.sqrt(6.0 / (fan_in + fan_out))
+    return torch.nn.Parameter(((torch.rand(fan_in, fan_out, generator=g) * 2 - 1) * a).cuda())
+
+
 class GCN(torch.nn.Module):
     """Two-layer GCN (Eq. 1): logits = A_hat ReLU(A_hat X W1) W2, each
     aggregation an AggregationLayer."""
@@ -223,13 +230,8 @@ class GCN(torch.nn.Module):
                  seed: int = 2, AT: DeviceCsr | None = None):
         super().__init__()
         g = torch.Generator().manual_seed(seed)
-
-        def glorot(fan_in, fan_out):
-            a = math.sqrt(6.0 / (fan_in + fan_out))
-            return torch.nn.Parameter(((torch.rand(fan_in, fan_out, generator=g) * 2 - 1) * a).cuda())
-
-        self.W1 = glorot(in_features, hidden)
-        self.W2 = glorot(hidden, classes)
+        self.W1 = _glorot(in_features, hidden, g)
+        self.W2 = _glorot(hidden, classes, g)
         self.agg1 = AggregationLayer(A, AT, hidden, cfg.refresh_interval)
         self.agg2 = AggregationLayer(A, AT, classes, cfg.refresh_interval)
         self.controller = RscController([self.agg1, self.agg2], cfg)
@@ -246,6 +248,59 @@ class GCN(torch.nn.Module):
             optimizer.zero_grad(set_to_none=True)
         logits = self(X)
         loss = torch.nn.functional.binary_cross_entropy_with_logits(logits, targets)
+        loss.backward()
+        self.controller.end(step)
+        if optimizer is not None:
+            optimizer.step()
+        return loss
+
+    def close(self):
+        self.controller.close()
+
+
+class GCNClassifier(torch.nn.Module):
+    """Residual GCN for single-label node classification, its update phase on
+    the library:
+
+        H_0 = ReLU(X W_in + b_in),  H_l = ReLU((A_hat H_{l-1}) W_l + b_l + H_{l-1}),
+        loss = mean over labelled nodes of softmax cross entropy of H_L W_out + b_out.
+
+    Each layer aggregates first, so that bias, residual and ReLU are the
+    epilogue of its product, every aggregation is `hidden` wide however many
+    classes there are, and the n x classes logits are never in memory."""
+
+    def __init__(self, A: DeviceCsr, in_features: int, hidden: int, classes: int, cfg: RscConfig, layers: int = 2,
+                 seed: int = 2, AT: DeviceCsr | None = None):
+        super().__init__()
+        if hidden % 4 or layers < 1:
+            raise ValueError(f"hidden {hidden}, layers {layers}: whole 16-byte rows and at least one layer expected")
+        g = torch.Generator().manual_seed(seed)
+        widths = [(in_features, hidden)] + [(hidden, hidden)] * layers + [(hidden, classes)]
+        self.weights = torch.nn.ParameterList([_glorot(a, b, g) for a, b in widths])
+        self.biases = torch.nn.ParameterList([torch.nn.Parameter(torch.zeros(b, device="cuda")) for _, b in widths])
+        self.aggregations = [AggregationLayer(A, AT, hidden, cfg.refresh_interval) for _ in range(layers)]
+        self.controller = RscController(self.aggregations, cfg)
+
+    def hidden(self, X: torch.Tensor) -> torch.Tensor:
+        H = linear(X, self.weights[0], self.biases[0], act="relu")
+        for agg, W, b in zip(self.aggregations, self.weights[1:], self.biases[1:]):
+            H = linear(agg(H), W, b, residual=H, act="relu")
+        return H
+
+    def forward(self, X: torch.Tensor) -> torch.Tensor:
+        """The logits (for evaluation)."""
+        return linear(self.hidden(X), self.weights[-1], self.biases[-1])
+
+    def loss(self, X: torch.Tensor, classes: torch.Tensor, ignore_index: int = -100) -> torch.Tensor:
+        return linear_cross_entropy(self.hidden(X), self.weights[-1], classes, self.biases[-1], ignore_index)
+
+    def train_step(self, X, classes, optimizer, step: int, ignore_index: int = -100):
+        """One RSC training step; classes: the nodes' classes, ignore_index for
+        nodes without a label."""
+        self.controller.begin(step)
+        if optimizer is not None:
+            optimizer.zero_grad(set_to_none=True)
+        loss = self.loss(X, classes, ignore_index)
         loss.backward()
         self.controller.end(step)
         if optimizer is not None:
