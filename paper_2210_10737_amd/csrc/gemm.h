@@ -9,21 +9,22 @@
 // (cols, cols) for dW = X^T dZ.
 //
 // One block computes a BM x BN tile with WM x WN waves, each a grid of 32x32
-// matrix-core tiles. The operands' tiles are BK = 128 bytes of k deep and go
-// from memory to LDS directly (16 bytes a lane, through buffer descriptors
-// that return zero past a matrix's end), double-buffered: the next tile is in
-// flight while the waves work on the present one.
+// matrix-core tiles. The operands' tiles are DEPTH bytes of k deep and go from
+// memory to LDS directly (16 bytes a lane, through buffer descriptors that
+// return zero past a matrix's end) into a ring of STAGES buffers.
 //
 // LDS layouts, both free of bank conflicts:
-//   kRows: 128 bytes a row, its eight 16-byte chunks at chunk ^ (row & 7); a
-//     lane reads its eight k values by one (fp32: two) 16-byte reads.
+//   kRows: DEPTH bytes a row, its 16-byte chunks XORed with a few bits of the
+//     row; a lane reads its eight k values by one (fp32: two) 16-byte reads.
 //   kCols: BK rows of BM (BN) values as they lie in memory, chunks XORed with
 //     a few bits of k; 16-bit fragments come by the transposing LDS read
 //     (ds_read_b64_tr_b16), fp32 ones by eight 4-byte reads.
 //
 // The matrix instruction is fed (B, A), so that a lane holds one row m and
-// four consecutive columns n per register quad: stores and row sums are along
-// n.
+// four consecutive columns n per register quad: row sums stay in the lane.
+// Results leave through LDS, 32 rows of a wave at a time, so that each store
+// (and each read of a residual) covers whole 128-byte lines: written straight
+// from the accumulators, 16 bytes a row, a 256 x 256 bf16 tile took 10 us more.
 //
 // fp32 operands: the fp32 matrix instruction runs at 1/16 of the bf16 one, so
 // each value is split into three bf16 parts (x = hi + mid + lo, exact for
@@ -60,7 +61,7 @@ constexpr uint32_t kOutside = 0x80000000u;  // past every descriptor's range
 // 16 bytes a lane from the descriptor's buffer to 64 consecutive places in LDS.
 // Written as assembly since the compiler waits for a load to LDS that it knows
 // of before the next LDS read, whichever buffer that is for; the load has no
-// register result, and wait_loads() stands before the barrier that hands a
+// register result, and wait_but() stands before the barrier that hands a
 // buffer over. (m0, the place in LDS, is a reserved register: the compiler
 // keeps nothing in it, and no other instruction of these kernels reads it.)
 __device__ __forceinline__ void load_to_lds(v4i rsrc, uint32_t lds, uint32_t off, uint32_t soff) {
@@ -72,7 +73,6 @@ __device__ __forceinline__ void load_to_lds(v4i rsrc, uint32_t lds, uint32_t off
         : "s"(lds), "v"(off), "s"(rsrc), "s"(soff)
         : "memory");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <typename T>
 struct Type;
@@ -95,17 +95,23 @@ struct Type<_Float16> {
     static __device__ __forceinline__ _Float16 put(float v) { return (_Float16)v; }
 };
 
-// ---- one operand's tile: R rows (or columns) by 128 bytes of k -------------
-template <typename T, bool COLS, int R, int WAVES>
+// ---- one operand's tile: R rows (or columns) by DEPTH bytes of k -----------
+template <typename T, bool COLS, int R, int WAVES, int DEPTH>
 struct Operand {
     static constexpr int ES = (int)sizeof(T);
-    static constexpr int BK = 128 / ES;
+    static constexpr int BK = DEPTH / ES;
     static constexpr int CH = 16 / ES;              // values a chunk
-    static constexpr int BYTES = R * 128;
+    static constexpr int BYTES = R * DEPTH;
     static constexpr int N = BYTES / 1024 / WAVES;  // loads of a wave
     static_assert(BYTES % (1024 * WAVES) == 0, "whole wave loads");
-    static constexpr int CPR = COLS ? R / CH : 8;   // chunks an LDS row
+    static_assert(WAVES % 2 == 0, "a lane's chunk of k is the same in all its loads");
+    static constexpr int CPR = COLS ? R / CH : DEPTH / 16;  // chunks an LDS row
 
+    // kRows: XOR of a chunk's place in its row. A 16-byte read takes 16 lanes,
+    // here 16 consecutive rows, a cycle from 64 banks: rows that start at the
+    // same bank (every second one of 128 bytes, every fourth of 64) get their
+    // chunk of k from different places.
+    static __device__ __forceinline__ int turn(int row) { return DEPTH == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
     // XOR of a chunk's place in LDS row k of the kCols form: 16 bits: four
     // rows of one transposing read fall into four 64-byte bank groups; fp32:
     // the two half-waves, eight rows apart, into two 128-byte ones
@@ -138,31 +144,39 @@ struct Operand {
             if (COLS)
                 off[q] = (uint32_t)(row * ldb) + (uint32_t)((slot ^ swizzle(row)) * 16);
             else
-                off[q] = (uint32_t)(row * ldb) + (uint32_t)((slot ^ (row & 7)) * 16);
+                off[q] = (uint32_t)(row * ldb) + (uint32_t)((slot ^ turn(row)) * 16);
         }
-        k_at = COLS ? 0 : ((lane & 7) ^ ((lane >> 3) & 7)) * CH;
+        k_at = COLS ? 0 : ((lane % CPR) ^ turn((wave * 64 + lane) / CPR)) * CH;
     }
 
-    // tile t's loads into LDS at `to`; last: it holds K's end
-    __device__ __forceinline__ void load(char *to, int t, int K, bool last, int wave) const {
+    // what a tile's loads share
+    struct Source {
+        v4i rsrc;
+        uint32_t soff;
+        bool outside;
+    };
+    // tile t; last: it holds K's end; !live: a tile past the end, its loads write zeros
+    __device__ __forceinline__ Source source(int t, int K, bool last, bool live) const {
         const char *from = base;
         int64_t left = bytes;
-        uint32_t so = 0;
+        Source o;
+        o.soff = 0;
         if (COLS) {
             from += t * step;
             left -= t * step;
         } else {
-            so = (uint32_t)t * 128u;
+            o.soff = (uint32_t)t * DEPTH;
         }
-        const uint32_t n = left <= 0 ? 0u : (uint32_t)(left < (int64_t)0x7ffffff0 ? left : (int64_t)0x7ffffff0);
+        const uint32_t n = left <= 0 || !live ? 0u : (uint32_t)(left < (int64_t)0x7ffffff0 ? left : (int64_t)0x7ffffff0);
         const uint64_t at = (uint64_t)from;
-        const v4i rs = {(int)(uint32_t)at, (int)(uint32_t)((at >> 32) & 0xffffu), (int)n, 0x00027000};
-        const bool outside = !COLS && last && t * BK + k_at >= K;
-#pragma unroll
-        for (int q = 0; q < N; ++q) {
-            const uint32_t o = outside ? kOutside : off[q];
-            load_to_lds(rs, (uint32_t)(uintptr_t)(lds_void *)(to + (q * WAVES + wave) * 1024), o, so);
-        }
+        o.rsrc = v4i{(int)(uint32_t)at, (int)(uint32_t)((at >> 32) & 0xffffu), (int)n, 0x00027000};
+        o.outside = !COLS && last && t * BK + k_at >= K;
+        return o;
+    }
+    // load q of the wave
+    __device__ __forceinline__ void load(const Source &o, int q, char *to, int wave) const {
+        load_to_lds(o.rsrc, (uint32_t)(uintptr_t)(lds_void *)(to + (q * WAVES + wave) * 1024),
+                    o.outside ? kOutside : off[q], o.soff);
     }
 
     // kRows, the tile that ends inside a chunk: zeroes that chunk's values from
@@ -170,7 +184,7 @@ struct Operand {
     static __device__ __forceinline__ void clear_tail(char *at, int kn, int threads) {
         if (COLS) return;
         for (int row = threadIdx.x; row < R; row += threads) {
-            T *chunk = (T *)(at + row * 128 + (((kn / CH) ^ (row & 7)) * 16));
+            T *chunk = (T *)(at + row * DEPTH + (((kn / CH) ^ turn(row)) * 16));
             for (int j = kn % CH; j < CH; ++j) chunk[j] = (T)0.f;
         }
     }
@@ -193,7 +207,7 @@ struct Operand {
                 f = __builtin_bit_cast(typename Type<T>::frag, v);
             } else {
                 const int row = r0 + (lane & 31), c = 2 * s + (lane >> 5);
-                f = *(const typename Type<T>::frag *)(at + row * 128 + ((c ^ (row & 7)) * 16));
+                f = *(const typename Type<T>::frag *)(at + row * DEPTH + ((c ^ turn(row)) * 16));
             }
         } else {
             if constexpr (COLS) {
@@ -205,8 +219,8 @@ struct Operand {
                 }
             } else {
                 const int row = r0 + (lane & 31), c = 4 * s + 2 * (lane >> 5);
-                const v4f a = *(const v4f *)(at + row * 128 + ((c ^ (row & 7)) * 16));
-                const v4f b = *(const v4f *)(at + row * 128 + (((c + 1) ^ (row & 7)) * 16));
+                const v4f a = *(const v4f *)(at + row * DEPTH + ((c ^ turn(row)) * 16));
+                const v4f b = *(const v4f *)(at + row * DEPTH + (((c + 1) ^ turn(row)) * 16));
                 f = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
             }
         }
@@ -240,52 +254,45 @@ struct Split {
 };
 
 // ---- the work of one block ------------------------------------------------
-template <typename T, bool AC, bool BC, int BM, int BN, int WM, int WN>
+// BM x BN by WM x WN waves, tiles DEPTH bytes of k deep, STAGES of them in LDS
+template <int BM_, int BN_, int WM_, int WN_, int DEPTH_, int STAGES_>
+struct Config {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_, STAGES = STAGES_;
+    static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
+};
+
+template <int N>
+__device__ __forceinline__ void wait_but() {  // all loads but the N youngest have landed
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <typename T, bool AC, bool BC, typename C>
 struct Tile {
-    static constexpr int WAVES = WM * WN;
-    static constexpr int THREADS = 64 * WAVES;
-    static constexpr int TA = BM / WM / 32, TB = BN / WN / 32;
-    using A = Operand<T, AC, BM, WAVES>;
-    using B = Operand<T, BC, BN, WAVES>;
-    static constexpr int BK = A::BK;
-    static constexpr int LDS = 2 * (A::BYTES + B::BYTES);
+    static constexpr int BM = C::BM, BN = C::BN, WN = C::WN, THREADS = C::THREADS, STAGES = C::STAGES;
+    static constexpr int TA = BM / C::WM / 32, TB = BN / WN / 32;
+    using A = Operand<T, AC, BM, C::WAVES, C::DEPTH>;
+    using B = Operand<T, BC, BN, C::WAVES, C::DEPTH>;
+    static constexpr int BK = A::BK, STEPS = BK / 16;
+    static_assert(STEPS % 2 == 0, "fragments alternate between two sets");
+    static constexpr int STAGE = A::BYTES + B::BYTES, LDS = STAGES * STAGE;
+    static constexpr int LOADS = A::N + B::N;  // of a wave for a tile
 
-    static __device__ __forceinline__ void compute(v16f (&acc)[TA][TB], const char *sa, const char *sb, int wm, int wn,
-                                                   int lane) {
-#pragma unroll
-        for (int s = 0; s < BK / 16; ++s) {
-            if constexpr (sizeof(T) == 2) {
-                typename Type<T>::frag a[TA], b[TB];
-#pragma unroll
-                for (int i = 0; i < TA; ++i) a[i] = A::frag(sa, (wm * TA + i) * 32, s, lane);
-#pragma unroll
-                for (int j = 0; j < TB; ++j) b[j] = B::frag(sb, (wn * TB + j) * 32, s, lane);
-#pragma unroll
-                for (int i = 0; i < TA; ++i)
-#pragma unroll
-                    for (int j = 0; j < TB; ++j) acc[i][j] = mfma(b[j], a[i], acc[i][j]);
-            } else {
-                v8bf b[TB][3];
-#pragma unroll
-                for (int j = 0; j < TB; ++j) {
-                    const Split v(B::frag(sb, (wn * TB + j) * 32, s, lane));
-#pragma unroll
-                    for (int u = 0; u < 3; ++u) b[j][u] = v.part[u];
-                }
-#pragma unroll
-                for (int i = 0; i < TA; ++i) {
-                    const Split a(A::frag(sa, (wm * TA + i) * 32, s, lane));
-                    constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
-#pragma unroll
-                    for (int u = 0; u < 6; ++u)
-#pragma unroll
-                        for (int j = 0; j < TB; ++j) acc[i][j] = mfma(b[j][pb[u]], a.part[pa[u]], acc[i][j]);
-                }
-            }
+    struct Frags {
+        typename Type<T>::frag a[TA], b[TB];
+        // fragment x of TA + TB, in the order in which multiply() needs them
+        __device__ __forceinline__ void read(int x, const char *at, int wm, int wn, int s, int lane) {
+            if (x == 0) a[0] = A::frag(at, wm * TA * 32, s, lane);
+            else if (x <= TB) b[x - 1] = B::frag(at + A::BYTES, (wn * TB + x - 1) * 32, s, lane);
+            else a[x - TB] = A::frag(at, (wm * TA + x - TB) * 32, s, lane);
         }
-    }
+    };
 
-    // acc = A(m0.., k) B(k, n0..) over the k tiles t0 .. t1 - 1
+    // acc = A(m0.., k) B(k, n0..) over the k tiles t0 .. t1 - 1. STAGES - 1
+    // tiles are in flight; the fragments of a step of 16 k are read while the
+    // step before is multiplied, across tiles too, and the loads of a later
+    // tile go out between the matrix instructions. For 16-bit operands the
+    // order is fixed by hand (a read or a load, then a matrix instruction):
+    // left to itself the compiler puts each read right before its use.
     static __device__ __forceinline__ void product(v16f (&acc)[TA][TB], const Product &p, char *lds, int m0, int n0,
                                                    int t0, int t1) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -300,26 +307,103 @@ struct Tile {
             for (int j = 0; j < TB; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        char *const la = lds, *const lb = lds + 2 * A::BYTES;
         const int last = (p.k - 1) / BK;
-        a.load(la, t0, p.k, t0 == last, wave);
-        b.load(lb, t0, p.k, t0 == last, wave);
-        int buf = 0;
-        for (int t = t0; t < t1; ++t) {
-            wait_loads();
-            __syncthreads();  // tile t has landed, and nobody reads the other buffer any more
-            const int nb = buf ^ 1;
-            if (t + 1 < t1) {
-                a.load(la + nb * A::BYTES, t + 1, p.k, t + 1 == last, wave);
-                b.load(lb + nb * B::BYTES, t + 1, p.k, t + 1 == last, wave);
-            }
-            if ((!AC || !BC) && t == last && p.k % A::CH != 0) {
-                A::clear_tail(la + buf * A::BYTES, p.k - t * BK, THREADS);
-                B::clear_tail(lb + buf * B::BYTES, p.k - t * BK, THREADS);
+        const bool cut = (!AC || !BC) && p.k % A::CH != 0 && t1 > last;  // K ends inside a chunk
+        // tile t is in LDS for every wave, and every wave is done with the one before
+        const auto arrive = [&](int t, char *at) {
+            wait_but<(STAGES - 2) * LOADS>();
+            __syncthreads();
+            if (cut && t == last) {
+                A::clear_tail(at, p.k - t * BK, THREADS);
+                B::clear_tail(at + A::BYTES, p.k - t * BK, THREADS);
                 __syncthreads();
             }
-            compute(acc, la + buf * A::BYTES, lb + buf * B::BYTES, wm, wn, lane);
-            buf = nb;
+        };
+        typename A::Source sa;
+        typename B::Source sb;
+        const auto aim = [&](int t) {
+            sa = a.source(t, p.k, t == last, t < t1);
+            sb = b.source(t, p.k, t == last, t < t1);
+        };
+        const auto load = [&](int x, char *to) {
+            if (x < A::N) a.load(sa, x, to, wave);
+            else b.load(sb, x - A::N, to + A::BYTES, wave);
+        };
+#pragma unroll
+        for (int u = 0; u < STAGES - 1; ++u) {
+            aim(t0 + u);
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) load(x, lds + u * STAGE);
+        }
+        char *at = lds, *const end = lds + STAGES * STAGE;
+        arrive(t0, at);
+        Frags f[2];
+#pragma unroll
+        for (int x = 0; x < TA + TB; ++x) f[0].read(x, at, wm, wn, 0, lane);
+        for (int t = t0; t < t1; ++t) {
+            char *const to = at == lds ? end - STAGE : at - STAGE;
+            char *const next = at + STAGE == end ? lds : at + STAGE;
+            aim(t + STAGES - 1);
+            // the tile's matrix instructions but the last step's, and how many of them pass between two loads
+            constexpr int MULS = TA * TB, ROOM = (STEPS - 1) * MULS, EVERY = STAGES > 2 && ROOM / LOADS > 1 ? ROOM / LOADS : 1;
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    const bool over = s + 1 == STEPS;  // reads on are the next tile's (zero or stale after the last)
+                    if (over) arrive(t + 1, next);
+#pragma unroll
+                    for (int x = 0; x < MULS; ++x) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        // reads in the first matrix instructions, evenly if there are more of them
+#pragma unroll
+                        for (int y = 0; y < TA + TB; ++y)
+                            if (y * MULS / (TA + TB > MULS ? TA + TB : MULS) == x)
+                                f[(s + 1) & 1].read(y, over ? next : at, wm, wn, over ? 0 : s + 1, lane);
+                        const int m = s * MULS + x;
+                        if (!over) {
+#pragma unroll
+                            for (int y = 0; y < LOADS; ++y)
+                                if (min(y * EVERY, ROOM - 1) == m) load(y, to);
+                        }
+                        acc[x / TB][x % TB] = mfma(f[s & 1].b[x % TB], f[s & 1].a[x / TB], acc[x / TB][x % TB]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < LOADS; ++x) load(x, to);
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    const bool over = s + 1 == STEPS;
+                    if (over) arrive(t + 1, next);
+#pragma unroll
+                    for (int x = 0; x < TA + TB; ++x)
+                        f[(s + 1) & 1].read(x, over ? next : at, wm, wn, over ? 0 : s + 1, lane);
+                    multiply_split(acc, f[s & 1]);
+                }
+            }
+            at = next;
+        }
+        wait_but<0>();
+        __syncthreads();  // nothing is in flight to LDS any more
+    }
+
+    static __device__ __forceinline__ void multiply_split(v16f (&acc)[TA][TB], const Frags &f) {
+        v8bf b[TB][3];
+#pragma unroll
+        for (int j = 0; j < TB; ++j) {
+            const Split v(f.b[j]);
+#pragma unroll
+            for (int u = 0; u < 3; ++u) b[j][u] = v.part[u];
+        }
+#pragma unroll
+        for (int i = 0; i < TA; ++i) {
+            const Split a(f.a[i]);
+            constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+            for (int u = 0; u < 6; ++u)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) acc[i][j] = mfma(b[j][pb[u]], a.part[pa[u]], acc[i][j]);
         }
     }
 };
@@ -362,146 +446,210 @@ __device__ __forceinline__ float exp_of(float x) {
 }
 
 template <typename T>
-__device__ __forceinline__ void load4(const T *p, int count, float (&v)[4]) {
-    typedef T v4 __attribute__((ext_vector_type(4)));
-    if (count >= 4) {
-        const v4 x = *(const v4 *)p;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = Type<T>::get(x[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < count ? Type<T>::get(p[i]) : 0.f;
-    }
-}
-template <typename T>
-__device__ __forceinline__ void store4(T *p, int count, const float (&v)[4]) {
-    typedef T v4 __attribute__((ext_vector_type(4)));
-    if (count >= 4) {
-        v4 x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = Type<T>::put(v[i]);
-        *(v4 *)p = x;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < count) p[i] = Type<T>::put(v[i]);
-    }
-}
-template <typename T>
 __device__ __forceinline__ float bias_at(const void *bias, int f32, int n) {
     return f32 ? ((const float *)bias)[n] : Type<T>::get(((const T *)bias)[n]);
 }
 
-// y = act(alpha acc + bias + beta r) of one 32x32 tile at (m0, n0)
+// values a lane takes of a row in the epilogue: 16 bytes of the result
 template <typename T>
-__device__ __forceinline__ void finish(const v16f &acc, const Product &p, const Epilogue &e, int m0, int n0, int lane) {
-    const int m = m0 + (lane & 31);
-    if (m >= p.m) return;
-    const float alpha = e.alpha_dev ? e.alpha * *e.alpha_dev : e.alpha;
+constexpr int kWidth = 16 / (int)sizeof(T);
+
+template <typename T>
+__device__ __forceinline__ void load_row(const T *p, int count, float (&v)[kWidth<T>]) {
+    constexpr int W = kWidth<T>;
+    typedef T vec __attribute__((ext_vector_type(W)));
+    if (count >= W) {
+        const vec x = *(const vec *)p;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int n = n0 + 8 * q + 4 * (lane >> 5), count = p.n - n;
-        if (count <= 0) continue;
-        float v[4];
+        for (int i = 0; i < W; ++i) v[i] = Type<T>::get(x[i]);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = alpha * acc[4 * q + i];
-        if (e.bias) {
+        for (int i = 0; i < W; ++i) v[i] = i < count ? Type<T>::get(p[i]) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_row(T *p, int count, const float (&v)[kWidth<T>]) {
+    constexpr int W = kWidth<T>;
+    typedef T vec __attribute__((ext_vector_type(W)));
+    if (count >= W) {
+        vec x;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < count) v[i] += bias_at<T>(e.bias, e.bias_f32, n + i);
+        for (int i = 0; i < W; ++i) x[i] = Type<T>::put(v[i]);
+        *(vec *)p = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (i < count) p[i] = Type<T>::put(v[i]);
+    }
+}
+// the same for W fp32 values at a place that is 16-byte aligned
+template <int W>
+__device__ __forceinline__ void load_f32(const float *p, int count, float (&v)[W]) {
+#pragma unroll
+    for (int q = 0; q < W / 4; ++q) {
+        float x[4];
+        load_row(p + 4 * q, count - 4 * q, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * q + i] = x[i];
+    }
+}
+template <int W>
+__device__ __forceinline__ void store_f32(float *p, int count, const float (&v)[W]) {
+#pragma unroll
+    for (int q = 0; q < W / 4; ++q) {
+        const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        store_row(p + 4 * q, count - 4 * q, x);
+    }
+}
+
+// the bias of a lane's columns, 0 without one or past the end
+template <typename T>
+__device__ __forceinline__ void load_bias(const void *bias, int f32, int n, int count, float (&v)[kWidth<T>]) {
+#pragma unroll
+    for (int i = 0; i < kWidth<T>; ++i) v[i] = bias && i < count ? bias_at<T>(bias, f32, n + i) : 0.f;
+}
+
+// y = act(alpha sum + bias + beta r) of row m, columns n .. n + count - 1
+template <typename T>
+__device__ __forceinline__ void finish(float (&v)[kWidth<T>], const float (&bias)[kWidth<T>], const Epilogue &e,
+                                       float alpha, int m, int n, int count) {
+    constexpr int W = kWidth<T>;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = fmaf(alpha, v[i], bias[i]);
+    if (e.r) {
+        float r[W];
+        if (e.r_f32) load_f32((const float *)e.r + (int64_t)m * e.ldr + n, count, r);
+        else load_row((const T *)e.r + (int64_t)m * e.ldr + n, count, r);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = fmaf(e.beta, r[i], v[i]);
+    }
+    if (e.pre) store_row((T *)e.pre + (int64_t)m * e.ldpre + n, count, v);
+    if (e.act != kNone) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = act_of(v[i], e.act);
+    }
+    if (e.y_f32) store_f32((float *)e.y + (int64_t)m * e.ldy + n, count, v);
+    else store_row((T *)e.y + (int64_t)m * e.ldy + n, count, v);
+}
+__device__ __forceinline__ float alpha_of(const Epilogue &e) { return e.alpha_dev ? e.alpha * *e.alpha_dev : e.alpha; }
+
+// f(i, m, n, v) for the accumulators' rows: W consecutive columns of a row a
+// call, a lane's column n the same in all calls. Through the wave's own part
+// of LDS, which nothing else uses then; rows are 16 bytes more than a multiple of 128
+// apart, so that 16 rows' writes and a row's reads fall into different banks.
+template <typename G, int W, typename F>
+__device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *lds, int m0, int n0, F f) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wm = wave / G::WN, wn = wave % G::WN;
+    constexpr int COLS = G::TB * 32, LD = COLS + 4;
+    static_assert(32 * LD * 4 * (G::THREADS / 64) <= G::LDS, "the waves' rows");
+    float *const slab = (float *)lds + wave * (32 * LD);
+    constexpr int LANES = COLS / W, ROWS = 64 / LANES;  // lanes a row, rows at a time
+    const int c = (lane % LANES) * W;
+#pragma unroll
+    for (int i = 0; i < G::TA; ++i) {
+#pragma unroll
+        for (int j = 0; j < G::TB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                v4f x;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = acc[i][j][4 * q + r];
+                *(v4f *)(slab + (lane & 31) * LD + j * 32 + 8 * q + 4 * (lane >> 5)) = x;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+        for (int u = 0; u < 32 / ROWS; ++u) {
+            const int row = u * ROWS + lane / LANES;
+            float v[W];
+#pragma unroll
+            for (int q = 0; q < W / 4; ++q) {
+                const v4f x = *(const v4f *)(slab + row * LD + c + 4 * q);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[4 * q + r] = x[r];
+            }
+            f(m0 + (wm * G::TA + i) * 32 + row, n0 + wn * COLS + c, v);
         }
-        if (e.r) {
-            float r[4];
-            if (e.r_f32)
-                load4((const float *)e.r + (int64_t)m * e.ldr + n, count, r);
-            else
-                load4((const T *)e.r + (int64_t)m * e.ldr + n, count, r);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = fmaf(e.beta, r[i], v[i]);
-        }
-        if (e.pre) store4((T *)e.pre + (int64_t)m * e.ldpre + n, count, v);
-        if (e.act != kNone) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], e.act);
-        }
-        if (e.y_f32)
-            store4((float *)e.y + (int64_t)m * e.ldy + n, count, v);
-        else
-            store4((T *)e.y + (int64_t)m * e.ldy + n, count, v);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
 // The product with the linear epilogue; with more than one split the raw sums
-// go to p.partial (in the order that the joining kernel reads them back).
-template <typename T, bool AC, bool BC, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM *WN, 1) void product_kernel(Product p, Epilogue e) {
-    using G = Tile<T, AC, BC, BM, BN, WM, WN>;
+// go to p.partial, a matrix of p.m rows ld_partial(p.n) apart for each split.
+__host__ __device__ inline int64_t ld_partial(int n) { return ((int64_t)n + 7) & ~(int64_t)7; }
+
+template <typename T, bool AC, bool BC, typename C>
+__global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilogue e) {
+    using G = Tile<T, AC, BC, C>;
+    constexpr int BM = C::BM, BN = C::BN, W = kWidth<T>;
     __shared__ __attribute__((aligned(1024))) char lds[G::LDS];
     const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     const Place o = place(tm, tn, p.splits);
     const int tiles = (p.k + G::BK - 1) / G::BK;
-    const int t0 = o.split * p.split_tiles, t1 = min(tiles, t0 + p.split_tiles);
+    const int t0 = o.split * (p.split_k / G::BK), t1 = min(tiles, t0 + p.split_k / G::BK);
     v16f acc[G::TA][G::TB];
     G::product(acc, p, lds, o.m * BM, o.n * BN, t0, t1);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wm = wave / WN, wn = wave % WN;
     if (p.splits > 1) {
-        float *to = p.partial + ((int64_t)o.split * tm * tn + o.m * tn + o.n) * (BM * BN);
-#pragma unroll
-        for (int i = 0; i < G::TA; ++i)
-#pragma unroll
-            for (int j = 0; j < G::TB; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v4f v;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
-                    const int sub = ((wm * G::TA + i) * (BN / 32) + wn * G::TB + j) * 4 + q;
-                    *(v4f *)(to + (int64_t)sub * 256 + lane * 4) = v;
-                }
+        float *const to = p.partial + (int64_t)o.split * p.m * ld_partial(p.n);
+        by_rows<G, 4>(acc, lds, o.m * BM, o.n * BN, [&](int m, int n, const float (&v)[4]) {
+            if (m < p.m && n < p.n) store_row(to + m * ld_partial(p.n) + n, p.n - n, v);
+        });
         return;
     }
-#pragma unroll
-    for (int i = 0; i < G::TA; ++i)
-#pragma unroll
-        for (int j = 0; j < G::TB; ++j)
-            finish<T>(acc[i][j], p, e, o.m * BM + (wm * G::TA + i) * 32, o.n * BN + (wn * G::TB + j) * 32, lane);
+    const float alpha = alpha_of(e);
+    float bias[W];
+    {
+        const int wn = (threadIdx.x >> 6) % G::WN, n = o.n * BN + wn * G::TB * 32 + ((threadIdx.x & 63) % (G::TB * 32 / W)) * W;
+        load_bias<T>(e.bias, e.bias_f32, n, p.n - n, bias);
+    }
+    by_rows<G, W>(acc, lds, o.m * BM, o.n * BN, [&](int m, int n, float (&v)[W]) {
+        if (m < p.m && n < p.n) finish<T>(v, bias, e, alpha, m, n, p.n - n);
+    });
 }
 
-// The sum of the splits' partial tiles, in split order, and the epilogue: a
-// wave for each 32x32 tile.
+// The sum of the splits' partial sums, in split order, and the epilogue: a
+// thread takes the W columns of one row.
 template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e, int bm, int bn) {
-    const int tm = (p.m + bm - 1) / bm, tn = (p.n + bn - 1) / bn;
-    const int sub_n = bn / 32, subs = (bm / 32) * sub_n;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (w >= (int64_t)tm * tn * subs) return;
-    const int tile = (int)(w / subs), sub = (int)(w % subs);
-    const int m0 = (tile / tn) * bm + (sub / sub_n) * 32, n0 = (tile % tn) * bn + (sub % sub_n) * 32;
-    if (m0 >= p.m || n0 >= p.n) return;
-    const float *from = p.partial + (int64_t)tile * (bm * bn) + sub * 1024 + lane * 4;
-    const int64_t step = (int64_t)tm * tn * bm * bn;
-    v16f acc;
+__global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
+    constexpr int W = kWidth<T>;
+    const int64_t ld = ld_partial(p.n), chunks = (p.n + W - 1) / W;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= chunks * p.m) return;
+    const int m = (int)(at / chunks), n = (int)(at % chunks) * W, count = p.n - n;
+    const float *from = p.partial + m * ld + n;
+    const int64_t step = (int64_t)p.m * ld;
+    float v[W], bias[W];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
+    for (int i = 0; i < W; ++i) v[i] = 0.f;
+    int s = 0;
+    for (; s + 4 <= p.splits; s += 4) {
+        float x[4][W];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const v4f v = *(const v4f *)(from + s * step + q * 256);
+        for (int u = 0; u < 4; ++u) load_f32(from + (s + u) * step, count, x[u]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[4 * q + r] += v[r];
-        }
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < W; ++i) v[i] += x[u][i];
     }
-    finish<T>(acc, p, e, m0, n0, lane);
+    for (; s < p.splits; ++s) {
+        float x[W];
+        load_f32(from + s * step, count, x);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] += x[i];
+    }
+    load_bias<T>(e.bias, e.bias_f32, n, count, bias);
+    finish<T>(v, bias, e, alpha_of(e), m, n, count);
 }
 
 // Softmax statistics of the logits X W + b over one tile of classes, for every
 // row the largest and the sum of exp(logit - largest): the logits stay in
 // registers. The lane that holds a row's own class writes its logit.
-template <typename T, bool BC, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM *WN, 1) void stats_kernel(Product p, Classes c) {
-    using G = Tile<T, false, BC, BM, BN, WM, WN>;
+template <typename T, bool BC, typename C>
+__global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes c) {
+    using G = Tile<T, false, BC, C>;
+    constexpr int BM = C::BM, BN = C::BN, WN = C::WN;
     __shared__ __attribute__((aligned(1024))) char lds[G::LDS];
     const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     const Place o = place(tm, tn, 1);
@@ -510,7 +658,6 @@ __global__ __launch_bounds__(64 * WM *WN, 1) void stats_kernel(Product p, Classe
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int wm = wave / WN, wn = wave % WN;
     float *const top = (float *)lds, *const sum = top + WN * BM;
-    __syncthreads();  // the operand tiles are read out
 #pragma unroll
     for (int i = 0; i < G::TA; ++i) {
         const int row = (wm * G::TA + i) * 32 + (lane & 31), m = o.m * BM + row;
@@ -557,39 +704,31 @@ __global__ __launch_bounds__(64 * WM *WN, 1) void stats_kernel(Product p, Classe
 
 // The logits' gradient over one piece of the classes, from recomputed logits:
 // g = weight (exp(logit - lse) - [own class]) c.scale, zero for rows left out.
-template <typename T, bool BC, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM *WN, 1) void grad_kernel(Product p, Classes c) {
-    using G = Tile<T, false, BC, BM, BN, WM, WN>;
+template <typename T, bool BC, typename C>
+__global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes c) {
+    using G = Tile<T, false, BC, C>;
+    constexpr int BM = C::BM, BN = C::BN, W = kWidth<T>;
     __shared__ __attribute__((aligned(1024))) char lds[G::LDS];
     const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     const Place o = place(tm, tn, 1);
     v16f acc[G::TA][G::TB];
     G::product(acc, p, lds, o.m * BM, o.n * BN, 0, (p.k + G::BK - 1) / G::BK);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wm = wave / WN, wn = wave % WN;
-#pragma unroll
-    for (int i = 0; i < G::TA; ++i) {
-        const int m = o.m * BM + (wm * G::TA + i) * 32 + (lane & 31);
-        if (m >= p.m) continue;
-        const int64_t t = c.target(m) - c.first;
+    float bias[W];
+    {
+        const int wn = (threadIdx.x >> 6) % G::WN, n = o.n * BN + wn * G::TB * 32 + ((threadIdx.x & 63) % (G::TB * 32 / W)) * W;
+        load_bias<T>(c.bias, c.bias_f32, n, p.n - n, bias);
+    }
+    by_rows<G, W>(acc, lds, o.m * BM, o.n * BN, [&](int m, int n, float (&v)[W]) {
+        if (m >= p.m || n >= p.n) return;
+        const int64_t t = c.target(m) - c.first - n;  // the own class among the lane's columns
         const float w = c.weight[m] * c.scale, lse = c.lse[m];
 #pragma unroll
-        for (int j = 0; j < G::TB; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = o.n * BN + (wn * G::TB + j) * 32 + 8 * q + 4 * (lane >> 5), count = p.n - n;
-                if (count <= 0) continue;
-                float v[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float l = acc[i][j][4 * q + r];
-                    if (c.bias && r < count) l += bias_at<T>(c.bias, c.bias_f32, n + r);
-                    const float g = w * (exp_of<T>(l - lse) - (n + r == t ? 1.f : 0.f));
-                    v[r] = w == 0.f ? 0.f : g;
-                }
-                store4((T *)c.grad + (int64_t)m * c.ldgrad + n, count, v);
-            }
-    }
+        for (int i = 0; i < W; ++i) {
+            const float g = w * (exp_of<T>(v[i] + bias[i] - lse) - (i == t ? 1.f : 0.f));
+            v[i] = w == 0.f ? 0.f : g;
+        }
+        store_row((T *)c.grad + (int64_t)m * c.ldgrad + n, p.n - n, v);
+    });
 }
 
 }  // namespace gemm

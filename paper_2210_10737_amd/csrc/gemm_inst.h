@@ -1,21 +1,27 @@
 // The launches of one operand type and layout: each gemm_*.hip defines RSC_T,
 // RSC_AC, RSC_BC (operands stored by columns) and RSC_NAME and includes this.
+#include <type_traits>
+
 #include "gemm.h"
 
 namespace rsc {
 namespace {
 
+// f(the shape's configuration). The largest has eight waves of 128 x 64 for 16
+// bits, and four of 128 x 128 for fp32, which split each value half as often
+// (8192^3: 209 TFLOP/s against 151 to 157 with eight). Tiles of 64 bytes of k
+// in a ring of four were within 4 % for 16 bits (1,259 against 1,231 at
+// 8192^3, 1,200 against 1,261 at 4096 x 4096 x 8192), and 16 % slower
+// where the operands' rows are 32 KiB apart.
 template <typename F>
 hipError_t with_shape(int shape, F f) {
+    using namespace gemm;
+    using Largest = std::conditional_t<sizeof(RSC_T) == 2, Config<256, 256, 2, 4, 128, 2>, Config<256, 256, 2, 2, 128, 2>>;
     switch (shape) {
-        case 0: return f(std::integral_constant<int, 256>(), std::integral_constant<int, 256>(),
-                         std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
-        case 1: return f(std::integral_constant<int, 128>(), std::integral_constant<int, 128>(),
-                         std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
-        case 2: return f(std::integral_constant<int, 128>(), std::integral_constant<int, 64>(),
-                         std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
-        case 3: return f(std::integral_constant<int, 32>(), std::integral_constant<int, 128>(),
-                         std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+        case 0: return f(Largest());
+        case 1: return f(Config<128, 128, 2, 2, 128, 2>());
+        case 2: return f(Config<128, 64, 2, 2, 128, 2>());
+        case 3: return f(Config<32, 128, 1, 4, 128, 4>());
     }
     return hipErrorInvalidValue;
 }
@@ -30,12 +36,12 @@ unsigned blocks_of(const Product &p, int bm, int bn) {
 #define RSC_CAT(a, b) RSC_CAT2(a, b)
 
 hipError_t RSC_CAT(product_, RSC_NAME)(int shape, const Product &p, const Epilogue &e, hipStream_t stream) {
-    return with_shape(shape, [&](auto bm, auto bn, auto wm, auto wn) {
-        gemm::product_kernel<RSC_T, RSC_AC, RSC_BC, bm.value, bn.value, wm.value, wn.value>
-            <<<blocks_of(p, bm.value, bn.value), 64 * wm.value * wn.value, 0, stream>>>(p, e);
+    return with_shape(shape, [&](auto config) {
+        using C = decltype(config);
+        gemm::product_kernel<RSC_T, RSC_AC, RSC_BC, C><<<blocks_of(p, C::BM, C::BN), C::THREADS, 0, stream>>>(p, e);
         if (p.splits > 1) {
-            const int64_t waves = ceil_div(p.m, bm.value) * ceil_div(p.n, bn.value) * (bm.value * bn.value / 1024);
-            gemm::join_kernel<RSC_T><<<(unsigned)ceil_div(waves, 4), 256, 0, stream>>>(p, e, bm.value, bn.value);
+            const int64_t threads = p.m * ceil_div(p.n, gemm::kWidth<RSC_T>);
+            gemm::join_kernel<RSC_T><<<(unsigned)ceil_div(threads, 256), 256, 0, stream>>>(p, e);
         }
         return hipGetLastError();
     });
@@ -43,16 +49,16 @@ hipError_t RSC_CAT(product_, RSC_NAME)(int shape, const Product &p, const Epilog
 
 #if !RSC_AC
 hipError_t RSC_CAT(stats_, RSC_NAME)(int shape, const Product &p, const Classes &c, hipStream_t stream) {
-    return with_shape(shape, [&](auto bm, auto bn, auto wm, auto wn) {
-        gemm::stats_kernel<RSC_T, RSC_BC, bm.value, bn.value, wm.value, wn.value>
-            <<<blocks_of(p, bm.value, bn.value), 64 * wm.value * wn.value, 0, stream>>>(p, c);
+    return with_shape(shape, [&](auto config) {
+        using C = decltype(config);
+        gemm::stats_kernel<RSC_T, RSC_BC, C><<<blocks_of(p, C::BM, C::BN), C::THREADS, 0, stream>>>(p, c);
         return hipGetLastError();
     });
 }
 hipError_t RSC_CAT(grad_, RSC_NAME)(int shape, const Product &p, const Classes &c, hipStream_t stream) {
-    return with_shape(shape, [&](auto bm, auto bn, auto wm, auto wn) {
-        gemm::grad_kernel<RSC_T, RSC_BC, bm.value, bn.value, wm.value, wn.value>
-            <<<blocks_of(p, bm.value, bn.value), 64 * wm.value * wn.value, 0, stream>>>(p, c);
+    return with_shape(shape, [&](auto config) {
+        using C = decltype(config);
+        gemm::grad_kernel<RSC_T, RSC_BC, C><<<blocks_of(p, C::BM, C::BN), C::THREADS, 0, stream>>>(p, c);
         return hipGetLastError();
     });
 }

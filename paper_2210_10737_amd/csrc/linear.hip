@@ -219,8 +219,8 @@ Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k) {
     };
     static const Rate kBf[kShapeCount] = {{5200, 1}, {4200, 2}, {2800, 3}, {1100, 4}};
     static const Rate kFp32[kShapeCount] = {{1000, 1}, {900, 2}, {700, 3}, {300, 4}};
-    const int64_t bk = dtype == kF32 ? 32 : 64, kt = ceil_div(k, bk);
-    Cut best{0, 1, (int32_t)kt, 0};
+    const int64_t bk = 128 / (int64_t)value_size(dtype), kt = ceil_div(k, bk);
+    Cut best{0, 1, (int32_t)(kt * bk), 0};
     double best_ns = 1e300;
     for (int s = 0; s < kShapeCount; ++s) {
         const Rate &r = dtype == kF32 ? kFp32[s] : kBf[s];
@@ -235,18 +235,15 @@ Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k) {
             const int64_t lone = std::min<int64_t>(r.per_cu, ceil_div(tiles * splits, kCus));
             const double share = std::max((double)lone / r.per_cu, 1.0 / 1.6);
             double ns = (rounds > 1 ? (double)rounds : share) * (double)per * step_ns + 1500.0;
-            if (splits > 1) ns += 2500.0 + 2.0 * 4.0 * (double)(tiles * kShapes[s].bm * kShapes[s].bn) * splits / 4000.0;
+            if (splits > 1) ns += 2500.0 + 2.0 * 4.0 * (double)m * (double)n * (double)splits / 4000.0;
             if (ns < best_ns) {
                 best_ns = ns;
-                best = Cut{s, (int32_t)splits, (int32_t)per, 0};
+                best = Cut{s, (int32_t)splits, (int32_t)(per * bk), 0};
             }
             if (tiles * splits > 4 * slots) break;  // more splits fill nothing
         }
     }
-    if (best.splits > 1) {
-        const Shape &sh = kShapes[best.shape];
-        best.bytes = sizeof(float) * (size_t)(ceil_div(m, sh.bm) * ceil_div(n, sh.bn)) * sh.bm * sh.bn * best.splits;
-    }
+    if (best.splits > 1) best.bytes = sizeof(float) * (size_t)best.splits * (size_t)m * (size_t)((n + 7) / 8 * 8);
     return best;
 }
 
@@ -261,7 +258,7 @@ hipError_t product_launch(int32_t dtype, int32_t layout, Product p, const Epilog
     if (p.m <= 0 || p.n <= 0) return hipSuccess;
     const Cut c = product_cut(dtype, p.m, p.n, p.k);
     p.splits = c.splits;
-    p.split_tiles = c.split_tiles;
+    p.split_k = c.split_k;
     p.partial = (float *)ws;
     using F = hipError_t (*)(int, const Product &, const Epilogue &, hipStream_t);
     static const F kProducts[3][3] = {{product_f32_rr, product_f32_rc, product_f32_cc},

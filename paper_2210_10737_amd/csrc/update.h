@@ -16,8 +16,9 @@ struct Product {
     const void *a = nullptr, *b = nullptr;
     int64_t lda = 0, ldb = 0;
     int32_t m = 0, n = 0, k = 0;
-    // the launch's own: k is cut into `splits` ranges of split_tiles tiles
-    int32_t splits = 1, split_tiles = 0;
+    // the launch's own: k is cut into `splits` ranges of split_k values, a
+    // multiple of every shape's tile
+    int32_t splits = 1, split_k = 0;
     float *partial = nullptr;
 };
 
@@ -89,7 +90,7 @@ RSC_CLASSES_DECL(f16_rr) RSC_CLASSES_DECL(f16_rc)
 // Tile shape and number of splits for a product of this size, and the bytes of
 // partial sums that the splits take (0 for one)
 struct Cut {
-    int32_t shape, splits, split_tiles;
+    int32_t shape, splits, split_k;
     size_t bytes;
 };
 Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k);
