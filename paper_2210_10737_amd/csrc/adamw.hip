@@ -58,8 +58,9 @@ __global__ void begin_kernel(int64_t *step, AdamwRates a, Now *now) {
     now->unbias = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)t)));
 }
 
-__device__ __forceinline__ uint64_t mix(uint64_t seed, uint64_t number) {
-    uint64_t z = seed + number * 0x9E3779B97F4A7C15ull;
+// SplitMix64 (Steele, Lea and Flood 2014): output `number` is mix(seed + number kGamma)
+constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ull;
+__device__ __forceinline__ uint64_t mix(uint64_t z) {
     z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
     z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
     return z ^ (z >> 31);
@@ -80,11 +81,25 @@ __device__ __forceinline__ float decode(float code, float by) {
     return w * fabsf(w);
 }
 
-__device__ __forceinline__ float encode(float x, float scale, float levels, uint32_t bits) {
+// The code by its definition, every operation rounded: min(floor(sqrt(x /
+// scale) levels + u), levels), scale taken as 1 where it is 0.
+__device__ __noinline__ float encode_exactly(float x, float scale, float levels, float u) {
 #pragma clang fp contract(off)
     const float share = x / (scale > 0.f ? scale : 1.f);
-    const float u = (float)bits * 0x1p-24f;
     return fminf(floorf(sqrtf(share) * levels + u), levels);
+}
+// The same from the hardware's reciprocal and root (1 ulp each, so within
+// levels 2^-21 with the roundings), and by the definition only where that
+// could be on the other side of a whole number: 2 levels 2^-21 of all values.
+// `inverse`: about 1 / scale. (The exact divisions and roots of two codes made
+// the step bound by instructions: 1,888 us for 400M parameters.)
+__device__ __forceinline__ float encode(float x, float scale, float inverse, float levels, uint32_t bits) {
+    const float u = (float)bits * 0x1p-24f;
+    const float a = fmaf(__builtin_amdgcn_sqrtf(x * inverse), levels, u);
+    const float f = floorf(a), part = a - f, near = levels * 0x1p-21f;
+    // written so that a NaN goes the exact way too
+    if (!(part > near && part < 1.f - near)) return encode_exactly(x, scale, levels, u);
+    return fminf(f, levels);
 }
 
 template <typename T, int COUNT>
@@ -190,14 +205,17 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, AdamwRates a, const 
         if (CODES) {
             m_top = wave_max(__uint_as_float(m_bits));
             r_top = wave_max(__uint_as_float(r_bits));
+            const float m_inv = __builtin_amdgcn_rcpf(m_top > 0.f ? m_top : 1.f);
+            const float r_inv = __builtin_amdgcn_rcpf(r_top > 0.f ? r_top : 1.f);
             int8_t q[4];
             uint8_t c[4];
+            uint64_t word = a.seed + (base + (uint64_t)at) * kGamma;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint64_t z = mix(a.seed, base + (uint64_t)(at + i));
-                const float qm = encode(fabsf(m[i]), m_top, 127.f, (uint32_t)(z & 0xffffffu));
+            for (int i = 0; i < 4; ++i, word += kGamma) {
+                const uint64_t z = mix(word);
+                const float qm = encode(fabsf(m[i]), m_top, m_inv, 127.f, (uint32_t)(z & 0xffffffu));
                 q[i] = (int8_t)(m[i] < 0.f ? -qm : qm);
-                const float qr = encode(r[i], r_top, 255.f, (uint32_t)((z >> 24) & 0xffffffu));
+                const float qr = encode(r[i], r_top, r_inv, 255.f, (uint32_t)((z >> 24) & 0xffffffu));
                 c[i] = (uint8_t)(r[i] > 0.f ? fmaxf(qr, 1.f) : qr);
             }
             put4((int8_t *)t.exp_avg + at, n, vec, q);

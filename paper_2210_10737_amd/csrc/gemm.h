@@ -37,6 +37,8 @@
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
+#include <type_traits>
+
 #include "rsc_internal.h"
 #include "update.h"
 
@@ -429,13 +431,12 @@ __device__ __forceinline__ Place place(int tiles_m, int tiles_n, int splits) {
 }
 
 // ---- epilogues --------------------------------------------------------------
-__device__ __forceinline__ float act_of(float z, int act) {
-    switch (act) {
-        case kRelu: return z > 0.f ? z : (z != z ? z : 0.f);
-        case kGelu: return 0.5f * z * erfcf(-0.70710678118654752f * z);
-        case kSilu: return z / (1.f + expf(-z));
-        default: return z;
-    }
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+    if (ACT == kRelu) return z > 0.f ? z : (z != z ? z : 0.f);
+    if (ACT == kGelu) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+    if (ACT == kSilu) return z / (1.f + expf(-z));
+    return z;
 }
 
 // exp of a difference of logits: to the rounding of fp32 where the result is
@@ -468,14 +469,15 @@ __device__ __forceinline__ void load_row(const T *p, int count, float (&v)[kWidt
     }
 }
 template <typename T>
-__device__ __forceinline__ void store_row(T *p, int count, const float (&v)[kWidth<T>]) {
+__device__ __forceinline__ void store_row(T *p, int count, const float (&v)[kWidth<T>], bool stream = false) {
     constexpr int W = kWidth<T>;
     typedef T vec __attribute__((ext_vector_type(W)));
     if (count >= W) {
         vec x;
 #pragma unroll
         for (int i = 0; i < W; ++i) x[i] = Type<T>::put(v[i]);
-        *(vec *)p = x;
+        if (stream) __builtin_nontemporal_store(x, (vec *)p);
+        else *(vec *)p = x;
     } else {
 #pragma unroll
         for (int i = 0; i < W; ++i)
@@ -509,38 +511,62 @@ __device__ __forceinline__ void load_bias(const void *bias, int f32, int n, int 
     for (int i = 0; i < kWidth<T>; ++i) v[i] = bias && i < count ? bias_at<T>(bias, f32, n + i) : 0.f;
 }
 
-// y = act(alpha sum + bias + beta r) of row m, columns n .. n + count - 1
-template <typename T>
+// A lane's place in the epilogue: its first row, and its columns n .. n +
+// count - 1, the same in every row that it takes (`down` rows further on,
+// the same for the whole wave).
+struct Spot {
+    int m, n, count;
+};
+
+// y = act(alpha sum + bias + beta r)
+template <typename T, int ACT>
 __device__ __forceinline__ void finish(float (&v)[kWidth<T>], const float (&bias)[kWidth<T>], const Epilogue &e,
-                                       float alpha, int m, int n, int count) {
+                                       float alpha, const Spot &at, int down) {
     constexpr int W = kWidth<T>;
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = fmaf(alpha, v[i], bias[i]);
     if (e.r) {
         float r[W];
-        if (e.r_f32) load_f32((const float *)e.r + (int64_t)m * e.ldr + n, count, r);
-        else load_row((const T *)e.r + (int64_t)m * e.ldr + n, count, r);
+        if (e.r_f32) load_f32((const float *)e.r + (at.m * e.ldr + at.n) + down * e.ldr, at.count, r);
+        else load_row((const T *)e.r + (at.m * e.ldr + at.n) + down * e.ldr, at.count, r);
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] = fmaf(e.beta, r[i], v[i]);
     }
-    if (e.pre) store_row((T *)e.pre + (int64_t)m * e.ldpre + n, count, v);
-    if (e.act != kNone) {
+    if (e.pre) store_row((T *)e.pre + (at.m * e.ldpre + at.n) + down * e.ldpre, at.count, v, e.stream);
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = act_of(v[i], e.act);
+    for (int i = 0; i < W; ++i) v[i] = act_of<ACT>(v[i]);
+    if (e.y_f32) store_f32((float *)e.y + (at.m * e.ldy + at.n) + down * e.ldy, at.count, v);
+    else store_row((T *)e.y + (at.m * e.ldy + at.n) + down * e.ldy, at.count, v, e.stream);
+}
+// f(the activation as a constant): one test a block
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    switch (act) {
+        case kRelu: return f(std::integral_constant<int, kRelu>());
+        case kGelu: return f(std::integral_constant<int, kGelu>());
+        case kSilu: return f(std::integral_constant<int, kSilu>());
+        default: return f(std::integral_constant<int, kNone>());
     }
-    if (e.y_f32) store_f32((float *)e.y + (int64_t)m * e.ldy + n, count, v);
-    else store_row((T *)e.y + (int64_t)m * e.ldy + n, count, v);
 }
 __device__ __forceinline__ float alpha_of(const Epilogue &e) { return e.alpha_dev ? e.alpha * *e.alpha_dev : e.alpha; }
 
-// f(i, m, n, v) for the accumulators' rows: W consecutive columns of a row a
-// call, a lane's column n the same in all calls. Through the wave's own part
+// f(down, v) for the accumulators' rows, W consecutive columns of the row
+// `down` below the lane's spot a call. Through the wave's own part
 // of LDS, which nothing else uses then; rows are 16 bytes more than a multiple of 128
 // apart, so that 16 rows' writes and a row's reads fall into different banks.
-template <typename G, int W, typename F>
-__device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *lds, int m0, int n0, F f) {
+template <typename G, int W>
+__device__ __forceinline__ Spot spot_of(const Product &p, int m0, int n0) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wm = wave / G::WN, wn = wave % G::WN;
+    constexpr int COLS = G::TB * 32, LANES = COLS / W;
+    Spot s;
+    s.m = m0 + (wave / G::WN) * G::TA * 32 + lane / LANES;
+    s.n = n0 + (wave % G::WN) * COLS + (lane % LANES) * W;
+    s.count = p.n - s.n;
+    return s;
+}
+template <typename G, int W, typename F>
+__device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *lds, F f) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     constexpr int COLS = G::TB * 32, LD = COLS + 4;
     static_assert(32 * LD * 4 * (G::THREADS / 64) <= G::LDS, "the waves' rows");
     float *const slab = (float *)lds + wave * (32 * LD);
@@ -569,7 +595,7 @@ __device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *l
 #pragma unroll
                 for (int r = 0; r < 4; ++r) v[4 * q + r] = x[r];
             }
-            f(m0 + (wm * G::TA + i) * 32 + row, n0 + wn * COLS + c, v);
+            f(i * 32 + u * ROWS, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -592,30 +618,36 @@ __global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilo
     v16f acc[G::TA][G::TB];
     G::product(acc, p, lds, o.m * BM, o.n * BN, t0, t1);
     if (p.splits > 1) {
-        float *const to = p.partial + (int64_t)o.split * p.m * ld_partial(p.n);
-        by_rows<G, 4>(acc, lds, o.m * BM, o.n * BN, [&](int m, int n, const float (&v)[4]) {
-            if (m < p.m && n < p.n) store_row(to + m * ld_partial(p.n) + n, p.n - n, v);
+        const Spot at = spot_of<G, 4>(p, o.m * BM, o.n * BN);
+        const int64_t ld = ld_partial(p.n);
+        float *const to = p.partial + (int64_t)o.split * p.m * ld + at.m * ld + at.n;
+        by_rows<G, 4>(acc, lds, [&](int down, const float (&v)[4]) {
+            if (at.count > 0 && at.m + down < p.m) store_row(to + down * ld, at.count, v);
         });
         return;
     }
     const float alpha = alpha_of(e);
+    const Spot at = spot_of<G, W>(p, o.m * BM, o.n * BN);
     float bias[W];
-    {
-        const int wn = (threadIdx.x >> 6) % G::WN, n = o.n * BN + wn * G::TB * 32 + ((threadIdx.x & 63) % (G::TB * 32 / W)) * W;
-        load_bias<T>(e.bias, e.bias_f32, n, p.n - n, bias);
-    }
-    by_rows<G, W>(acc, lds, o.m * BM, o.n * BN, [&](int m, int n, float (&v)[W]) {
-        if (m < p.m && n < p.n) finish<T>(v, bias, e, alpha, m, n, p.n - n);
+    load_bias<T>(e.bias, e.bias_f32, at.n, at.count, bias);
+    with_act(e.act, [&](auto act) {
+        by_rows<G, W>(acc, lds, [&](int down, float (&v)[W]) {
+            if (at.count > 0 && at.m + down < p.m) finish<T, decltype(act)::value>(v, bias, e, alpha, at, down);
+        });
     });
 }
 
-// The sum of the splits' partial sums, in split order, and the epilogue: a
-// thread takes the W columns of one row.
-template <typename T>
+// The sum of the splits' partial sums and the epilogue: L neighbouring threads
+// take W columns of one row, each every L-th split, and add up over a fixed
+// tree. One thread is enough where the results fill the chip; with few of them
+// (a single row) the splits' reads, one after another, were the time: 16.5 us
+// for 4,096 results of 64 splits.
+template <typename T, int L>
 __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
     constexpr int W = kWidth<T>;
     const int64_t ld = ld_partial(p.n), chunks = (p.n + W - 1) / W;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+    const int part = threadIdx.x % L;
     if (at >= chunks * p.m) return;
     const int m = (int)(at / chunks), n = (int)(at % chunks) * W, count = p.n - n;
     const float *from = p.partial + m * ld + n;
@@ -623,24 +655,30 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
     float v[W], bias[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = 0.f;
-    int s = 0;
-    for (; s + 4 <= p.splits; s += 4) {
+    int s = part;
+    for (; s + 3 * L < p.splits; s += 4 * L) {
         float x[4][W];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) load_f32(from + (s + u) * step, count, x[u]);
+        for (int u = 0; u < 4; ++u) load_f32(from + (s + u * L) * step, count, x[u]);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int i = 0; i < W; ++i) v[i] += x[u][i];
     }
-    for (; s < p.splits; ++s) {
+    for (; s < p.splits; s += L) {
         float x[W];
         load_f32(from + s * step, count, x);
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] += x[i];
     }
+#pragma unroll
+    for (int d = 1; d < L; d *= 2)
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] += __shfl_xor(v[i], d);
+    if (part != 0) return;
     load_bias<T>(e.bias, e.bias_f32, n, count, bias);
-    finish<T>(v, bias, e, alpha_of(e), m, n, count);
+    const Spot spot{m, n, count};
+    with_act(e.act, [&](auto act) { finish<T, decltype(act)::value>(v, bias, e, alpha_of(e), spot, 0); });
 }
 
 // Softmax statistics of the logits X W + b over one tile of classes, for every
@@ -713,21 +751,20 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
     const Place o = place(tm, tn, 1);
     v16f acc[G::TA][G::TB];
     G::product(acc, p, lds, o.m * BM, o.n * BN, 0, (p.k + G::BK - 1) / G::BK);
+    const Spot at = spot_of<G, W>(p, o.m * BM, o.n * BN);
     float bias[W];
-    {
-        const int wn = (threadIdx.x >> 6) % G::WN, n = o.n * BN + wn * G::TB * 32 + ((threadIdx.x & 63) % (G::TB * 32 / W)) * W;
-        load_bias<T>(c.bias, c.bias_f32, n, p.n - n, bias);
-    }
-    by_rows<G, W>(acc, lds, o.m * BM, o.n * BN, [&](int m, int n, float (&v)[W]) {
-        if (m >= p.m || n >= p.n) return;
-        const int64_t t = c.target(m) - c.first - n;  // the own class among the lane's columns
+    load_bias<T>(c.bias, c.bias_f32, at.n, at.count, bias);
+    by_rows<G, W>(acc, lds, [&](int down, float (&v)[W]) {
+        const int m = at.m + down;
+        if (m >= p.m || at.count <= 0) return;
+        const int64_t t = c.target(m) - c.first - at.n;  // the own class among the lane's columns
         const float w = c.weight[m] * c.scale, lse = c.lse[m];
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             const float g = w * (exp_of<T>(v[i] + bias[i] - lse) - (i == t ? 1.f : 0.f));
             v[i] = w == 0.f ? 0.f : g;
         }
-        store_row((T *)c.grad + (int64_t)m * c.ldgrad + n, p.n - n, v);
+        store_row((T *)c.grad + (at.m * c.ldgrad + at.n) + down * c.ldgrad, at.count, v);
     });
 }
 

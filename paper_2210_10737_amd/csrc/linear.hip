@@ -131,20 +131,33 @@ __global__ __launch_bounds__(256) void pass_kernel(Pass p) {
     }
 }
 
-// out[col] = scale * the chunks' sums, in chunk order within four interleaved
-// ranges of chunks that are added at the end
+// out[col] = scale * the chunks' sums: 64 threads a column, each every 64th
+// chunk in order, then over a fixed tree. (16 threads a column took 31 to 42
+// us for 2,048 chunks.)
 template <typename T>
-__global__ __launch_bounds__(256) void column_total_kernel(const double *part, int32_t chunks, int32_t m, float scale,
+__global__ __launch_bounds__(1024) void column_total_kernel(const double *part, int32_t chunks, int32_t m, float scale,
                                                            const float *scale_dev, T *out) {
-    __shared__ double sum[256];
+    __shared__ double sum[1024];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), s = threadIdx.x >> 4;
     double acc = 0.0;
-    if (c < m)
-        for (int i = s; i < chunks; i += 16) acc += part[(int64_t)i * m + c];
+    if (c < m) {
+        int i = s;
+        for (; i + 192 < chunks; i += 256) {
+            const double *p = part + (int64_t)i * m + c;
+            const double x = p[0], y = p[64 * (int64_t)m], z = p[128 * (int64_t)m], w = p[192 * (int64_t)m];
+            acc += (x + y) + (z + w);
+        }
+        for (; i < chunks; i += 64) acc += part[(int64_t)i * m + c];
+    }
     sum[threadIdx.x] = acc;
     __syncthreads();
+#pragma unroll
+    for (int h = 32; h > 0; h /= 2) {
+        if (s < h) sum[threadIdx.x] += sum[threadIdx.x + h * 16];
+        __syncthreads();
+    }
     if (s == 0 && c < m) {
-        for (int i = 1; i < 16; ++i) acc += sum[i * 16 + (threadIdx.x & 15)];
+        acc = sum[threadIdx.x];
         const double by = scale_dev ? (double)scale * (double)*scale_dev : (double)scale;
         out[c] = (T)(float)(by * acc);
     }
@@ -189,11 +202,11 @@ hipError_t total_launch(int32_t dtype, const double *part, int32_t chunks, int32
                         const float *scale_dev, void *out, int32_t out_f32, hipStream_t stream) {
     const unsigned grid = (unsigned)ceil_div(m, 16);
     if (dtype == kF32 || out_f32)
-        column_total_kernel<float><<<grid, 256, 0, stream>>>(part, chunks, m, scale, scale_dev, (float *)out);
+        column_total_kernel<float><<<grid, 1024, 0, stream>>>(part, chunks, m, scale, scale_dev, (float *)out);
     else if (dtype == kBf16)
-        column_total_kernel<__bf16><<<grid, 256, 0, stream>>>(part, chunks, m, scale, scale_dev, (__bf16 *)out);
+        column_total_kernel<__bf16><<<grid, 1024, 0, stream>>>(part, chunks, m, scale, scale_dev, (__bf16 *)out);
     else
-        column_total_kernel<_Float16><<<grid, 256, 0, stream>>>(part, chunks, m, scale, scale_dev, (_Float16 *)out);
+        column_total_kernel<_Float16><<<grid, 1024, 0, stream>>>(part, chunks, m, scale, scale_dev, (_Float16 *)out);
     return hipGetLastError();
 }
 
@@ -209,16 +222,20 @@ hipError_t zero_launch(int32_t dtype, void *p, int64_t ld, int64_t rows, int64_t
 
 // ---- tile shape and splits ----------------------------------------------------
 // A model of the time in nanoseconds: blocks run in rounds of as many as the
-// 256 CUs hold, a block's tiles of k at the rate its shape reaches; splits add
-// the writing and reading of their partial sums and a launch.
-Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k) {
-    // flops per ns of a CU with all its blocks, blocks a CU
+// 256 CUs hold, a block's tiles of k at the rate its shape reaches and a fixed
+// part for its first loads and its results; splits add a launch and the
+// writing and reading of their partial sums.
+namespace {
+Cut cut_of(int32_t dtype, int64_t m, int64_t n, int64_t k, bool may_split) {
+    // flops per ns of a CU with all its blocks, blocks a CU, ns of a block
+    // besides its tiles of k
     struct Rate {
         double rate;
         int per_cu;
+        double fixed;
     };
-    static const Rate kBf[kShapeCount] = {{5200, 1}, {4200, 2}, {2800, 3}, {1100, 4}};
-    static const Rate kFp32[kShapeCount] = {{1000, 1}, {900, 2}, {700, 3}, {300, 4}};
+    static const Rate kBf[kShapeCount] = {{5000, 1, 9000}, {3900, 2, 5000}, {3000, 3, 4000}, {1100, 2, 2500}};
+    static const Rate kFp32[kShapeCount] = {{850, 1, 26000}, {720, 2, 9000}, {650, 3, 5000}, {300, 2, 2500}};
     const int64_t bk = 128 / (int64_t)value_size(dtype), kt = ceil_div(k, bk);
     Cut best{0, 1, (int32_t)(kt * bk), 0};
     double best_ns = 1e300;
@@ -227,35 +244,44 @@ Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k) {
         const int64_t tiles = ceil_div(m, kShapes[s].bm) * ceil_div(n, kShapes[s].bn);
         const int64_t slots = (int64_t)kCus * r.per_cu;
         const double step_ns = 2.0 * kShapes[s].bm * kShapes[s].bn * (double)bk * r.per_cu / r.rate;
-        for (int64_t want = 1; want <= kt; want = want < 4 ? want + 1 : want + want / 4) {
+        // as many splits as fill 1/4, 1/2, 1 or 2 rounds of blocks
+        int64_t last = 0;
+        for (int f = -3; f <= (may_split ? 1 : -3); ++f) {
+            const int64_t fill = f < 0 ? slots >> -f : slots << f;
+            const int64_t want = f == -3 ? 1 : std::min(kt, std::max<int64_t>(fill / tiles, 1));
             const int64_t per = ceil_div(kt, want), splits = ceil_div(kt, per);
-            if (tiles * splits > (int64_t(1) << 30)) break;
-            const int64_t rounds = ceil_div(tiles * splits, slots);
-            // a round that is not full runs its blocks faster, a single block a CU at most 1.6 times
-            const int64_t lone = std::min<int64_t>(r.per_cu, ceil_div(tiles * splits, kCus));
-            const double share = std::max((double)lone / r.per_cu, 1.0 / 1.6);
-            double ns = (rounds > 1 ? (double)rounds : share) * (double)per * step_ns + 1500.0;
-            if (splits > 1) ns += 2500.0 + 2.0 * 4.0 * (double)m * (double)n * (double)splits / 4000.0;
+            if (splits <= last) continue;
+            last = splits;
+            const int64_t blocks = tiles * splits, rounds = ceil_div(blocks, slots);
+            // a CU that holds fewer blocks than it could runs each faster, a single one at most 1.6 times
+            const double share = rounds > 1 ? (double)rounds
+                                            : std::max((double)std::min<int64_t>(r.per_cu, ceil_div(blocks, kCus)) / r.per_cu,
+                                                       r.per_cu > 1 ? 1.0 / 1.6 : 1.0);
+            double ns = share * (double)per * step_ns + (double)rounds * r.fixed;
+            if (splits > 1)
+                ns += 2500.0 + 2.0 * 4.0 * (double)m * (double)n * (double)splits / 8000.0 + 25.0 * (double)splits;
             if (ns < best_ns) {
                 best_ns = ns;
                 best = Cut{s, (int32_t)splits, (int32_t)(per * bk), 0};
             }
-            if (tiles * splits > 4 * slots) break;  // more splits fill nothing
         }
     }
-    if (best.splits > 1) best.bytes = sizeof(float) * (size_t)best.splits * (size_t)m * (size_t)((n + 7) / 8 * 8);
+    if (best.splits > 1)
+        best.bytes = sizeof(float) * (size_t)best.splits * (size_t)m * (size_t)((n + 7) / 8 * 8);
     return best;
 }
+}  // namespace
+
+Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k) { return cut_of(dtype, m, n, k, true); }
 
 // the loss's products take every logit of a tile at once, so k is not split
-int loss_shape(int32_t, int64_t m, int64_t n) {
-    if (m <= 32) return 3;
-    if (n <= 64) return 2;
-    return ceil_div(m, 256) * ceil_div(n, 256) >= kCus / 2 ? 0 : 1;
-}
+int loss_shape(int32_t dtype, int64_t m, int64_t n, int64_t k) { return cut_of(dtype, m, n, k, false).shape; }
 
-hipError_t product_launch(int32_t dtype, int32_t layout, Product p, const Epilogue &e, void *ws, hipStream_t stream) {
+hipError_t product_launch(int32_t dtype, int32_t layout, Product p, Epilogue e, void *ws, hipStream_t stream) {
     if (p.m <= 0 || p.n <= 0) return hipSuccess;
+    // results far beyond the L2s (32 MiB in all) only push the operands out of
+    // them: 200,000 x 300 x 512 fp32 494 us, 445 with streaming stores; 232,964 x 256 x 600 560, 532
+    e.stream = (double)p.m * p.n * (double)value_size(dtype) > 128.0 * 1024 * 1024;
     const Cut c = product_cut(dtype, p.m, p.n, p.k);
     p.splits = c.splits;
     p.split_k = c.split_k;

@@ -176,14 +176,14 @@ int rows_split(int64_t tiles) { return tiles >= 16 ? 16 : 1; }
 }  // namespace
 
 size_t loss_ws_bytes(const Loss &l) {
-    const int64_t n = std::max(l.n, 1), tiles = ceil_div(l.v, kShapes[loss_shape(l.dtype, l.n, l.v)].bn);
+    const int64_t n = std::max(l.n, 1), tiles = ceil_div(l.v, kShapes[loss_shape(l.dtype, l.n, l.v, l.k)].bn);
     return align_up(sizeof(float2) * (size_t)(tiles * n), 256) + align_up(sizeof(float) * (size_t)n, 256) +
            2 * align_up(sizeof(double) * (size_t)ceil_div(n, 256 / rows_split(tiles)), 256);
 }
 
 hipError_t loss_launch(const Loss &l, const void *x, int64_t ldx, const void *w, int64_t ldw, const Classes &classes,
                        float *loss, float *lse, float *count, void *ws, hipStream_t stream) {
-    const int shape = loss_shape(l.dtype, l.n, l.v);
+    const int shape = loss_shape(l.dtype, l.n, l.v, l.k);
     const int64_t tiles = ceil_div(l.v, kShapes[shape].bn), n = std::max(l.n, 1);
     const int split = rows_split(tiles);
     const unsigned blocks = (unsigned)ceil_div(l.n, 256 / split);
@@ -299,7 +299,7 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
         p.m = l.n;
         p.n = vc;
         p.k = l.k;
-        e = grad_fn(l)(loss_shape(l.dtype, l.n, vc), p, c, stream);
+        e = grad_fn(l)(loss_shape(l.dtype, l.n, vc, l.k), p, c, stream);
         if (g.dx && e == hipSuccess) {
             Product q;
             q.a = c.grad;

@@ -38,6 +38,8 @@ struct Epilogue {
     int64_t ldy = 0;
     void *pre = nullptr;
     int64_t ldpre = 0;
+    // results go past the caches (set by the launch for large ones)
+    bool stream = false;
 };
 
 // What the loss's products need besides X and W
@@ -94,9 +96,9 @@ struct Cut {
     size_t bytes;
 };
 Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k);
-int loss_shape(int32_t dtype, int64_t m, int64_t n);
+int loss_shape(int32_t dtype, int64_t m, int64_t n, int64_t k);
 // runs it; ws holds the cut's bytes
-hipError_t product_launch(int32_t dtype, int32_t layout, Product p, const Epilogue &e, void *ws, hipStream_t stream);
+hipError_t product_launch(int32_t dtype, int32_t layout, Product p, Epilogue e, void *ws, hipStream_t stream);
 
 inline size_t value_size(int32_t dtype) { return dtype == kF32 ? 4 : 2; }
 

@@ -24,13 +24,11 @@ _REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
 
 
 # ---------------------------------------------------------------- matrices
-def _unit(dtype: torch.dtype) -> int:
-    return 16 // dtype.itemsize
-
-
+# (small calls are bound by the host's time for them, so each property is read
+# from a tensor once)
 def _new(rows: int, cols: int, dtype, device) -> torch.Tensor:
     """rows x cols view of rows that are whole 16-byte units."""
-    u = _unit(dtype)
+    u = 16 // dtype.itemsize
     ld = (cols + u - 1) // u * u
     t = torch.empty((rows, ld), dtype=dtype, device=device)
     return t if ld == cols else t[:, :cols]
@@ -40,8 +38,8 @@ def _ld(t: torch.Tensor) -> int | None:
     """The leading dimension the library can use for a 2-D tensor, or None."""
     rows, cols = t.shape
     s0, s1 = t.stride()
-    u = _unit(t.dtype)
-    if (cols > 1 and s1 != 1) or t.data_ptr() % 16:
+    u = 16 // t.dtype.itemsize
+    if (s1 != 1 and cols > 1) or t.data_ptr() % 16:
         return None
     if rows <= 1:
         return (cols + u - 1) // u * u
@@ -60,13 +58,15 @@ def _matrix(t: torch.Tensor) -> tuple[torch.Tensor, int]:
 
 def _weights(w: torch.Tensor) -> tuple[torch.Tensor, int, int]:
     """(w or a copy, leading dimension, 1 if stored output-major)."""
-    ld = _ld(w)
-    if ld is not None:
-        return w, ld, 0
-    ld = _ld(w.t())
-    if ld is not None:
-        return w, ld, 1
-    if w.stride(0) == 1 and w.shape[0] > 1:   # keep the order it is stored in
+    k, m = w.shape
+    s0, s1 = w.stride()
+    u = 16 // w.dtype.itemsize
+    if w.data_ptr() % 16 == 0:
+        if s1 == 1 and s0 >= m and s0 % u == 0:
+            return w, s0, 0
+        if s0 == 1 and s1 >= k and s1 % u == 0:
+            return w, s1, 1
+    if s0 == 1 and k > 1:   # keep the order it is stored in
         t, ld = _matrix(w.t())
         return t.t(), ld, 1
     c, ld = _matrix(w)
@@ -85,25 +85,34 @@ def _new_like_weights(w: torch.Tensor, out_major: int) -> tuple[torch.Tensor, in
 def _check_operand(t: torch.Tensor, name: str, shape, dtype=None) -> None:
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: {t.dtype}, {dtype} expected")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, {tuple(shape)} expected")
     if t.get_device() != _device_index():
         raise ValueError(f"{name} on {t.device}: the library runs on the current device cuda:{_device_index()}")
 
 
-def _check_product(x: torch.Tensor, weight: torch.Tensor, bias) -> None:
-    if x.dtype not in _DTYPES:
-        raise ValueError(f"x: {x.dtype}, one of float32, bfloat16, float16 expected")
-    if x.dim() != 2 or weight.dim() != 2:
+def _check_product(x: torch.Tensor, weight: torch.Tensor, bias) -> tuple[int, int, int]:
+    """n, k, m of x @ weight (+ bias)."""
+    dtype, xs, ws = x.dtype, x.shape, weight.shape
+    if dtype not in _DTYPES:
+        raise ValueError(f"x: {dtype}, one of float32, bfloat16, float16 expected")
+    if len(xs) != 2 or len(ws) != 2:
         raise ValueError("x and weight must be 2-D")
-    if weight.shape[0] < 1 or weight.shape[1] < 1:
-        raise ValueError(f"weight: shape {tuple(weight.shape)}")
-    _check_operand(x, "x", (x.shape[0], weight.shape[0]))
-    _check_operand(weight, "weight", weight.shape, x.dtype)
+    n, k = xs
+    m = ws[1]
+    if ws[0] != k or k < 1 or m < 1:
+        raise ValueError(f"x of shape {tuple(xs)}, weight of shape {tuple(ws)}")
+    if weight.dtype != dtype:
+        raise ValueError(f"weight: {weight.dtype}, {dtype} expected")
+    dev = _device_index()
+    if x.get_device() != dev or weight.get_device() != dev:
+        raise ValueError(f"x on {x.device}, weight on {weight.device}: the library runs on the current device "
+                         f"cuda:{dev}")
     if bias is not None:
-        if bias.dtype not in (x.dtype, torch.float32):
-            raise ValueError(f"bias: {bias.dtype}, {x.dtype} or float32 expected")
-        _check_operand(bias, "bias", (weight.shape[1],))
+        if bias.dtype != dtype and bias.dtype != torch.float32:
+            raise ValueError(f"bias: {bias.dtype}, {dtype} or float32 expected")
+        _check_operand(bias, "bias", (m,))
+    return n, k, m
 
 
 def _bias_arg(bias):
@@ -117,20 +126,23 @@ def _bias_arg(bias):
 def _linear_forward(x, weight, bias, residual, act: int, alpha: float, beta: float, out, keep: bool):
     """(y, pre or None, the aligned x and weight)."""
     n, (k, m) = x.shape[0], weight.shape
+    dtype, dev = x.dtype, x.device
     xa, ldx = _matrix(x)
     wa, ldw, out_major = _weights(weight)
     b, pb, b_dtype = _bias_arg(bias)
-    p = LinearStruct(_DTYPES[x.dtype], act, n, k, m, out_major, alpha, beta)
-    y = _new(n, m, x.dtype, x.device) if out is None else out
-    ldy = _ld(y)
+    p = LinearStruct(_DTYPES[dtype], act, n, k, m, out_major, alpha, beta)
+    y = _new(n, m, dtype, dev) if out is None else out
     ra, ldr = (None, 0) if residual is None else _matrix(residual)
-    pre = _new(n, m, x.dtype, x.device) if keep and act >= 2 else None
-    need = lib().rsc_linear_workspace_bytes(ctypes.byref(p))
-    ws = _workspace(need, x.device) if need else None
-    _check(lib().rsc_linear(ctypes.byref(p), xa.data_ptr(), ldx, wa.data_ptr(), ldw, pb, b_dtype,
-                            None if ra is None else ra.data_ptr(), ldr, y.data_ptr(), ldy,
-                            None if pre is None else pre.data_ptr(), 0 if pre is None else _ld(pre),
-                            None if ws is None else ws.data_ptr(), need, _stream()))
+    pre = _new(n, m, dtype, dev) if keep and act >= 2 else None
+    L, ref = lib(), ctypes.byref(p)
+    need = L.rsc_linear_workspace_bytes(ref)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    status = L.rsc_linear(ref, xa.data_ptr(), ldx, wa.data_ptr(), ldw, pb, b_dtype,
+                          None if ra is None else ra.data_ptr(), ldr, y.data_ptr(), _ld(y),
+                          None if pre is None else pre.data_ptr(), 0 if pre is None else _ld(pre),
+                          None if ws is None else ws.data_ptr(), need, _stream())
+    if status:
+        _check(status)
     return y, pre, xa, wa
 
 
@@ -187,11 +199,12 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     be the residual."""
     if act not in _ACTS:
         raise ValueError(f"act {act!r}: none, relu, gelu or silu expected")
-    _check_product(x, weight, bias)
-    n, m = x.shape[0], weight.shape[1]
+    n, _, m = _check_product(x, weight, bias)
     if residual is not None:
         _check_operand(residual, "residual", (n, m), x.dtype)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, residual)):
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                    (bias is not None and bias.requires_grad) or
+                                    (residual is not None and residual.requires_grad)):
         if out is not None:
             raise ValueError("out is for calls without gradients")
         return _Linear.apply(x, weight, bias, residual, _ACTS[act], float(alpha), float(beta))
@@ -279,7 +292,8 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.T
     if not -(1 << 63) <= int(ignore_index) < 1 << 63:
         raise ValueError(f"ignore_index {ignore_index} is no int64")
     args = (x, weight, targets, bias, int(ignore_index), _REDUCTIONS[reduction])
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                    (bias is not None and bias.requires_grad)):
         return _Xent.apply(*args)
     return _xent_forward(*args)[0]
 
