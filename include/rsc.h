@@ -509,7 +509,8 @@ rsc_status_t rsc_greedy_allocate_profiles(int32_t L, int32_t n, int64_t nnz, int
  *   - Matrices are row-major with a leading dimension ld (in values); a row
  *     is a whole number of 16 bytes (ld * size % 16 == 0) of at most 4 MiB
  *     and the base pointer is 16-byte aligned. What lies between a row's last
- *     value and the next row is not used and, in outputs, not written.
+ *     value and the next row is not used (up to the end of its 16 bytes it may
+ *     be read) and, in outputs, not written.
  *   - Vectors (bias, its gradient) are contiguous, of the operands' type or,
  *     with bias_dtype RSC_F32, fp32.
  *   - Workspaces are 256-byte aligned and private to the call until it

@@ -455,18 +455,15 @@ __device__ __forceinline__ float bias_at(const void *bias, int f32, int n) {
 template <typename T>
 constexpr int kWidth = 16 / (int)sizeof(T);
 
+// the first `count` (at least 1) of a row's 16 bytes, zeros behind them. All
+// are read: rows are whole 16-byte units apart, so they lie with the first one.
 template <typename T>
 __device__ __forceinline__ void load_row(const T *p, int count, float (&v)[kWidth<T>]) {
     constexpr int W = kWidth<T>;
     typedef T vec __attribute__((ext_vector_type(W)));
-    if (count >= W) {
-        const vec x = *(const vec *)p;
+    const vec x = *(const vec *)p;
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = Type<T>::get(x[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = i < count ? Type<T>::get(p[i]) : 0.f;
-    }
+    for (int i = 0; i < W; ++i) v[i] = i < count ? Type<T>::get(x[i]) : 0.f;
 }
 template <typename T>
 __device__ __forceinline__ void store_row(T *p, int count, const float (&v)[kWidth<T>], bool stream = false) {
@@ -489,8 +486,8 @@ template <int W>
 __device__ __forceinline__ void load_f32(const float *p, int count, float (&v)[W]) {
 #pragma unroll
     for (int q = 0; q < W / 4; ++q) {
-        float x[4];
-        load_row(p + 4 * q, count - 4 * q, x);
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        if (count > 4 * q) load_row(p + 4 * q, count - 4 * q, x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[4 * q + i] = x[i];
     }
@@ -681,6 +678,83 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
     with_act(e.act, [&](auto act) { finish<T, decltype(act)::value>(v, bias, e, alpha_of(e), spot, 0); });
 }
 
+// Few rows (R of them, 1 to kFewRows) against weights stored by rows: bound by
+// reading the weights once, so a wave takes two columns, 16 bytes of their rows
+// a lane and turn, sums in the lane and then over a fixed tree. Neither tiles nor
+// splits nor a joining launch: 4096 x 4096 bf16 (33.5 MB of weights) one row
+// 5.3 us against 9.4 by tiles, two 9.5 against 10.4; 4096 x 4096 fp32 12.3
+// against 19.6 and 13.2 against 20. fp32 operands are multiplied as they are.
+template <typename T, int R>
+__global__ __launch_bounds__(256) void few_rows_kernel(Product p, Epilogue e) {
+    constexpr int W = kWidth<T>, AHEAD = 4, COLUMNS = 2;
+    typedef T vec __attribute__((ext_vector_type(W)));
+    const int n0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * COLUMNS, lane = threadIdx.x & 63;
+    if (n0 >= p.n) return;
+    const T *w[COLUMNS];
+#pragma unroll
+    for (int j = 0; j < COLUMNS; ++j) w[j] = (const T *)p.b + min(n0 + j, p.n - 1) * p.ldb;
+    float acc[COLUMNS][R];
+#pragma unroll
+    for (int j = 0; j < COLUMNS; ++j)
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[j][r] = 0.f;
+    int k0 = lane * W;
+    for (; k0 + (AHEAD - 1) * 64 * W + W <= p.k; k0 += 64 * W * AHEAD) {
+        vec a[AHEAD][R], b[AHEAD][COLUMNS];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+#pragma unroll
+            for (int j = 0; j < COLUMNS; ++j) b[u][j] = *(const vec *)(w[j] + k0 + u * 64 * W);
+#pragma unroll
+            for (int r = 0; r < R; ++r) a[u][r] = *(const vec *)((const T *)p.a + r * p.lda + k0 + u * 64 * W);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < COLUMNS; ++j)
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+                        acc[j][r] = fmaf(Type<T>::get(a[u][r][i]), Type<T>::get(b[u][j][i]), acc[j][r]);
+    }
+    for (; k0 < p.k; k0 += 64 * W) {
+        float b[COLUMNS][W];
+#pragma unroll
+        for (int j = 0; j < COLUMNS; ++j) load_row(w[j] + k0, p.k - k0, b[j]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float a[W];
+            load_row((const T *)p.a + r * p.lda + k0, p.k - k0, a);
+#pragma unroll
+            for (int j = 0; j < COLUMNS; ++j)
+#pragma unroll
+                for (int i = 0; i < W; ++i) acc[j][r] = fmaf(a[i], b[j][i], acc[j][r]);
+        }
+    }
+    // lane j R + r finishes column j of row r
+    float v = 0.f;
+#pragma unroll
+    for (int j = 0; j < COLUMNS; ++j)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int d = 32; d > 0; d /= 2) acc[j][r] += __shfl_xor(acc[j][r], d);
+            if (lane == j * R + r) v = acc[j][r];
+        }
+    const int n = n0 + lane / R, m = lane % R;
+    if (lane >= COLUMNS * R || n >= p.n) return;
+    v = fmaf(alpha_of(e), v, e.bias ? bias_at<T>(e.bias, e.bias_f32, n) : 0.f);
+    if (e.r) {
+        const int64_t at = m * e.ldr + n;
+        v = fmaf(e.beta, e.r_f32 ? ((const float *)e.r)[at] : Type<T>::get(((const T *)e.r)[at]), v);
+    }
+    if (e.pre) ((T *)e.pre)[m * e.ldpre + n] = Type<T>::put(v);
+    with_act(e.act, [&](auto act) { v = act_of<decltype(act)::value>(v); });
+    if (e.y_f32) ((float *)e.y)[m * e.ldy + n] = v;
+    else ((T *)e.y)[m * e.ldy + n] = Type<T>::put(v);
+}
+
 // Softmax statistics of the logits X W + b over one tile of classes, for every
 // row the largest and the sum of exp(logit - largest): the logits stay in
 // registers. The lane that holds a row's own class writes its logit.
@@ -696,23 +770,35 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int wm = wave / WN, wn = wave % WN;
     float *const top = (float *)lds, *const sum = top + WN * BM;
+    const int n0 = o.n * BN + wn * G::TB * 32 + 4 * (lane >> 5);  // column of a lane's r = 0, j = 0
+    const bool whole = o.n * BN + BN <= p.n;
+    float bias[G::TB][16];
+#pragma unroll
+    for (int j = 0; j < G::TB; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int n = n0 + j * 32 + 8 * (r >> 2) + (r & 3);
+            // what is past the last class takes no part
+            bias[j][r] = n >= p.n ? -INFINITY : c.bias ? bias_at<T>(c.bias, c.bias_f32, n) : 0.f;
+        }
 #pragma unroll
     for (int i = 0; i < G::TA; ++i) {
         const int row = (wm * G::TA + i) * 32 + (lane & 31), m = o.m * BM + row;
         const int64_t t = m < p.m ? c.target(m) : -1;
-        float mx = -INFINITY;
+        // the own class, counted from n0, if it is one of this lane's columns
+        const int at = t >= n0 && t < n0 + G::TB * 32 && t < p.n && (((t - n0) >> 2) & 1) == 0 ? (int)(t - n0) : -1;
+        float mx = -INFINITY, own = 0.f;
 #pragma unroll
         for (int j = 0; j < G::TB; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int n = o.n * BN + (wn * G::TB + j) * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
                 float v = acc[i][j][r];
-                if (c.bias && n < p.n) v += bias_at<T>(c.bias, c.bias_f32, n);
-                if (n >= p.n) v = -INFINITY;
-                else if (n == t) c.own_logit[m] = v;
+                if (c.bias || !whole) v = bias[j][r] == -INFINITY ? -INFINITY : v + bias[j][r];
+                if (at == j * 32 + 8 * (r >> 2) + (r & 3)) own = v;
                 acc[i][j][r] = v;
                 mx = fmaxf(mx, v);
             }
+        if (at >= 0) c.own_logit[m] = own;
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         float s = 0.f;
         const float base = mx == -INFINITY ? 0.f : mx;  // no class left: exp(-inf) = 0 each

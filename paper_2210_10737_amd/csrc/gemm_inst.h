@@ -36,6 +36,17 @@ unsigned blocks_of(const Product &p, int bm, int bn) {
 #define RSC_CAT(a, b) RSC_CAT2(a, b)
 
 hipError_t RSC_CAT(product_, RSC_NAME)(int shape, const Product &p, const Epilogue &e, hipStream_t stream) {
+#if !RSC_AC && !RSC_BC
+    if (shape == kFewRowsShape) {
+        const unsigned blocks = (unsigned)ceil_div(p.n, 8);
+        switch (p.m) {
+            case 1: gemm::few_rows_kernel<RSC_T, 1><<<blocks, 256, 0, stream>>>(p, e); break;
+            case 2: gemm::few_rows_kernel<RSC_T, 2><<<blocks, 256, 0, stream>>>(p, e); break;
+            default: return hipErrorInvalidValue;
+        }
+        return hipGetLastError();
+    }
+#endif
     return with_shape(shape, [&](auto config) {
         using C = decltype(config);
         gemm::product_kernel<RSC_T, RSC_AC, RSC_BC, C><<<blocks_of(p, C::BM, C::BN), C::THREADS, 0, stream>>>(p, e);

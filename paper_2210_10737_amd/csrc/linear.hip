@@ -59,62 +59,66 @@ struct Pass {
 };
 
 template <typename T>
-__global__ __launch_bounds__(256) void pass_kernel(Pass p) {
+__device__ __forceinline__ void write_row(T *p, int count, const float (&v)[Val<T>::W], float by) {
     constexpr int W = Val<T>::W;
     typedef T vec __attribute__((ext_vector_type(W)));
+    if (count >= W) {
+        vec x;
+#pragma unroll
+        for (int i = 0; i < W; ++i) x[i] = (T)(by * v[i]);
+        *(vec *)p = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (i < count) p[i] = (T)(by * v[i]);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void pass_kernel(Pass p) {
+    constexpr int W = Val<T>::W;
     __shared__ double sum[256 * W];
     const int g = threadIdx.x & (p.groups - 1), lanes = 256 / p.groups, lane = threadIdx.x / p.groups;
-    const int c = (blockIdx.y * p.groups + g) * W, count = p.m - c;
-    const int64_t r0 = (int64_t)blockIdx.x * p.rows_a_chunk, r1 = min(p.n, r0 + p.rows_a_chunk);
+    const int c = (blockIdx.x * p.groups + g) * W, count = p.m - c;
+    const int64_t r0 = (int64_t)blockIdx.y * p.rows_a_chunk, r1 = min(p.n, r0 + p.rows_a_chunk);
     double acc[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) acc[i] = 0.0;
     if (count > 0) {
-        for (int64_t r = r0 + lane; r < r1; r += lanes) {
-            float v[W];
-            const T *py = (const T *)p.dy + r * p.lddy + c;
-            if (count >= W) {
-                const vec x = *(const vec *)py;
-#pragma unroll
-                for (int i = 0; i < W; ++i) v[i] = (float)x[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < W; ++i) v[i] = i < count ? (float)py[i] : 0.f;
-            }
+        const auto take = [&](int64_t row, float (&v)[W], const float (&s)[W]) {
             if (p.act != kNone) {
-                const T *ps = (const T *)p.saved + r * p.ldsaved + c;
-                float s[W];
-                if (count >= W) {
-                    const vec x = *(const vec *)ps;
-#pragma unroll
-                    for (int i = 0; i < W; ++i) s[i] = (float)x[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < W; ++i) s[i] = i < count ? (float)ps[i] : 0.f;
-                }
 #pragma unroll
                 for (int i = 0; i < W; ++i) v[i] *= slope_of(s[i], p.act);
             }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                T *to = k == 0 ? (T *)p.dz : (T *)p.dr;
-                if (!to) continue;
-                to += r * (k == 0 ? p.lddz : p.lddr) + c;
-                const float by = k == 0 ? 1.f : p.beta;
-                if (count >= W) {
-                    vec x;
-#pragma unroll
-                    for (int i = 0; i < W; ++i) x[i] = (T)(by * v[i]);
-                    *(vec *)to = x;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < W; ++i)
-                        if (i < count) to[i] = (T)(by * v[i]);
-                }
-            }
+            if (p.dz) write_row<T>((T *)p.dz + row * p.lddz + c, count, v, 1.f);
+            if (p.dr) write_row<T>((T *)p.dr + row * p.lddr + c, count, v, p.beta);
             if (p.part) {
 #pragma unroll
                 for (int i = 0; i < W; ++i) acc[i] += (double)v[i];
+            }
+        };
+        // four rows a turn, all read before the first is converted or anything
+        // is written. Whole 16 bytes are read also where the row ends inside
+        // them (rows are whole 16-byte units apart) and zeroed from there on.
+        typedef T vec __attribute__((ext_vector_type(W)));
+        for (int64_t r = r0 + lane; r < r1; r += 4 * lanes) {
+            vec y[4], z[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t row = min(r + u * lanes, r1 - 1);
+                y[u] = *(const vec *)((const T *)p.dy + row * p.lddy + c);
+                if (p.act != kNone) z[u] = *(const vec *)((const T *)p.saved + row * p.ldsaved + c);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (r + u * lanes >= r1) break;
+                float v[W], s[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    v[i] = i < count ? (float)y[u][i] : 0.f;
+                    s[i] = p.act != kNone && i < count ? (float)z[u][i] : 0.f;
+                }
+                take(r + u * lanes, v, s);
             }
         }
     }
@@ -123,11 +127,11 @@ __global__ __launch_bounds__(256) void pass_kernel(Pass p) {
     for (int i = 0; i < W; ++i) sum[i * 256 + threadIdx.x] = acc[i];
     __syncthreads();
     for (int j = threadIdx.x; j < p.groups * W; j += 256) {
-        const int col = (blockIdx.y * p.groups) * W + j;
+        const int col = (blockIdx.x * p.groups) * W + j;
         if (col >= p.m) continue;
         double s = 0.0;
         for (int l = 0; l < lanes; ++l) s += sum[(j % W) * 256 + l * p.groups + j / W];
-        p.part[(int64_t)blockIdx.x * p.m + col] = s;
+        p.part[(int64_t)blockIdx.y * p.m + col] = s;
     }
 }
 
@@ -191,7 +195,9 @@ Chunks chunks_of(int32_t dtype, int64_t n, int64_t m) {
 hipError_t pass_launch(int32_t dtype, Pass p, const Chunks &c, hipStream_t stream) {
     p.groups = c.groups;
     p.rows_a_chunk = c.rows;
-    const dim3 grid((unsigned)c.count, (unsigned)c.strips);
+    // a row's strips next to each other: blocks that run together read whole
+    // rows (strips of rows 4 KiB apart alone are in a quarter of the channels)
+    const dim3 grid((unsigned)c.strips, (unsigned)c.count);
     if (dtype == kF32) pass_kernel<float><<<grid, 256, 0, stream>>>(p);
     else if (dtype == kBf16) pass_kernel<__bf16><<<grid, 256, 0, stream>>>(p);
     else pass_kernel<_Float16><<<grid, 256, 0, stream>>>(p);
@@ -272,7 +278,10 @@ Cut cut_of(int32_t dtype, int64_t m, int64_t n, int64_t k, bool may_split) {
 }
 }  // namespace
 
-Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k) { return cut_of(dtype, m, n, k, true); }
+Cut product_cut(int32_t dtype, int32_t layout, int64_t m, int64_t n, int64_t k) {
+    if (layout == kRowsRows && m <= kFewRows) return Cut{kFewRowsShape, 1, 0, 0};
+    return cut_of(dtype, m, n, k, true);
+}
 
 // the loss's products take every logit of a tile at once, so k is not split
 int loss_shape(int32_t dtype, int64_t m, int64_t n, int64_t k) { return cut_of(dtype, m, n, k, false).shape; }
@@ -282,7 +291,7 @@ hipError_t product_launch(int32_t dtype, int32_t layout, Product p, Epilogue e, 
     // results far beyond the L2s (32 MiB in all) only push the operands out of
     // them: 200,000 x 300 x 512 fp32 494 us, 445 with streaming stores; 232,964 x 256 x 600 560, 532
     e.stream = (double)p.m * p.n * (double)value_size(dtype) > 128.0 * 1024 * 1024;
-    const Cut c = product_cut(dtype, p.m, p.n, p.k);
+    const Cut c = product_cut(dtype, layout, p.m, p.n, p.k);
     p.splits = c.splits;
     p.split_k = c.split_k;
     p.partial = (float *)ws;
@@ -294,7 +303,9 @@ hipError_t product_launch(int32_t dtype, int32_t layout, Product p, Epilogue e, 
 }
 
 // ---- layer ----------------------------------------------------------------------
-size_t linear_ws_bytes(const Linear &l) { return align_up(product_cut(l.dtype, l.n, l.m, l.k).bytes, 256); }
+size_t linear_ws_bytes(const Linear &l) {
+    return align_up(product_cut(l.dtype, l.out_major ? kRowsRows : kRowsCols, l.n, l.m, l.k).bytes, 256);
+}
 
 hipError_t linear_launch(const Linear &l, const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias,
                          int32_t bias_f32, const void *r, int64_t ldr, void *y, int64_t ldy, void *pre, int64_t ldpre,
@@ -330,9 +341,9 @@ size_t dz_bytes(const Linear &l) {
 }
 size_t cut_bytes(const Linear &l, bool dx, bool dw) {
     size_t b = 0;
-    if (dx) b = std::max(b, product_cut(l.dtype, l.n, l.k, l.m).bytes);
-    if (dw) b = std::max(b, l.out_major ? product_cut(l.dtype, l.m, l.k, l.n).bytes
-                                        : product_cut(l.dtype, l.k, l.m, l.n).bytes);
+    if (dx) b = std::max(b, product_cut(l.dtype, l.out_major ? kRowsCols : kRowsRows, l.n, l.k, l.m).bytes);
+    if (dw) b = std::max(b, l.out_major ? product_cut(l.dtype, kColsCols, l.m, l.k, l.n).bytes
+                                        : product_cut(l.dtype, kColsCols, l.k, l.m, l.n).bytes);
     return align_up(b, 256);
 }
 }  // namespace

@@ -153,12 +153,15 @@ __global__ __launch_bounds__(256) void weight_kernel(Classes c, const float *dlo
 
 constexpr size_t kPieceBytes = size_t(256) << 20;
 
-// classes of a piece: a multiple of 256 such that G stays near 256 MiB, at
-// least 2,048, at most a row of G's 4 MiB
+// classes of a piece: a multiple of 256 such that G stays within 256 MiB, or
+// 2,048 where that is more, and a row of G within 4 MiB; all pieces alike, since a
+// small last one would leave most of the chip idle
 int64_t piece_of(const Loss &l) {
     const int64_t row = (int64_t)std::max(l.n, 1) * (int64_t)value_size(l.dtype);
     const int64_t fit = (int64_t)kPieceBytes / row / 256 * 256;
-    return std::min<int64_t>(l.v, std::min<int64_t>(std::max<int64_t>(fit, 2048), int64_t(1) << 20));
+    const int64_t most = std::min<int64_t>(std::max<int64_t>(fit, 2048), int64_t(1) << 20);
+    if (l.v <= most) return l.v;
+    return (int64_t)align_up((size_t)ceil_div(l.v, ceil_div(l.v, most)), 256);
 }
 
 using StatsFn = hipError_t (*)(int, const Product &, const Classes &, hipStream_t);
@@ -233,9 +236,9 @@ size_t piece_cuts(const Loss &l, bool dx, bool dw) {
     size_t b = 0;
     for (int64_t v : {piece, rest}) {
         if (v == 0) continue;
-        if (dx) b = std::max(b, product_cut(l.dtype, l.n, l.k, v).bytes);
-        if (dw) b = std::max(b, l.out_major ? product_cut(l.dtype, v, l.k, l.n).bytes
-                                            : product_cut(l.dtype, l.k, v, l.n).bytes);
+        if (dx) b = std::max(b, product_cut(l.dtype, l.out_major ? kRowsCols : kRowsRows, l.n, l.k, v).bytes);
+        if (dw) b = std::max(b, l.out_major ? product_cut(l.dtype, kColsCols, v, l.k, l.n).bytes
+                                            : product_cut(l.dtype, kColsCols, l.k, v, l.n).bytes);
     }
     return align_up(b, 256);
 }

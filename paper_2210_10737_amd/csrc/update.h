@@ -74,6 +74,8 @@ struct Shape {
 };
 constexpr Shape kShapes[] = {{256, 256}, {128, 128}, {128, 64}, {32, 128}};
 constexpr int kShapeCount = 4;
+// a kernel of its own: up to this many rows against weights stored by rows
+constexpr int kFewRowsShape = 4, kFewRows = 2;
 
 #define RSC_PRODUCT_DECL(name)                                                                       \
     hipError_t product_##name(int shape, const Product &p, const Epilogue &e, hipStream_t stream);
@@ -95,7 +97,7 @@ struct Cut {
     int32_t shape, splits, split_k;
     size_t bytes;
 };
-Cut product_cut(int32_t dtype, int64_t m, int64_t n, int64_t k);
+Cut product_cut(int32_t dtype, int32_t layout, int64_t m, int64_t n, int64_t k);
 int loss_shape(int32_t dtype, int64_t m, int64_t n, int64_t k);
 // runs it; ws holds the cut's bytes
 hipError_t product_launch(int32_t dtype, int32_t layout, Product p, Epilogue e, void *ws, hipStream_t stream);
