@@ -582,20 +582,26 @@ typedef struct {
 
 /* rsc_xent: loss (fp32; 1 value, or n with reduction 0), lse (n values: log
  * sum exp of each row's logits) and count (1 value: what the loss was divided
- * by; unused with reduction 0) are outputs that the backward pass reads. */
+ * by; unused with reduction 0) are outputs that the backward pass reads.
+ * G (n x v of the operands' type, nullable; only with v <= 64 and reduction 1
+ * or 2, else RSC_ERR_UNSUPPORTED) receives the logits' gradient for an
+ * upstream gradient of one a row (fp16: times 1,024), for a backward pass that
+ * then need not form the logits again. */
 size_t rsc_xent_workspace_bytes(const rsc_xent_t *p);
 rsc_status_t rsc_xent(const rsc_xent_t *p, const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias,
-                      const void *targets, float *loss, float *lse, float *count, void *ws, size_t ws_bytes,
-                      hipStream_t stream);
+                      const void *targets, float *loss, float *lse, float *count, void *G, int64_t ldg, void *ws,
+                      size_t ws_bytes, hipStream_t stream);
 /* Gradients for dloss (device, fp32; 1 value, or n with reduction 0): dX (n x
- * k), dW (stored as W is) and dbias, each may be NULL. The workspace holds
- * one piece of the logits' gradient (256 MiB, or n x 2,048 values where that
- * is more) and, with more than one piece, dX in fp32. */
-size_t rsc_xent_backward_workspace_bytes(const rsc_xent_t *p, int32_t with_dx, int32_t with_dw);
+ * k), dW (stored as W is) and dbias, each may be NULL. G: what rsc_xent wrote
+ * there for the same arguments, or NULL: the logits are then formed again. The
+ * workspace holds one piece of the logits' gradient (256 MiB, or n x 2,048
+ * values where that is more; none with G) and, with more than one piece, dX in
+ * fp32. */
+size_t rsc_xent_backward_workspace_bytes(const rsc_xent_t *p, int32_t with_dx, int32_t with_dw, int32_t with_g);
 rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const void *X, int64_t ldx, const void *W,
                                int64_t ldw, const void *bias, const void *targets, const float *lse,
-                               const float *count, void *dX, int64_t lddx, void *dW, int64_t lddw, void *dbias,
-                               void *ws, size_t ws_bytes, hipStream_t stream);
+                               const float *count, const void *G, int64_t ldg, void *dX, int64_t lddx, void *dW,
+                               int64_t lddw, void *dbias, void *ws, size_t ws_bytes, hipStream_t stream);
 
 /* One AdamW step over `count` tensors:
  *   t = ++*step;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2

@@ -191,11 +191,11 @@ def lib():
             "rsc_linear_backward": ([ctypes.POINTER(LinearStruct), vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp,
                                      i64, vp, i32, vp, i64, vp, sz, vp], ctypes.c_int),
             "rsc_xent_workspace_bytes": ([ctypes.POINTER(XentStruct)], sz),
-            "rsc_xent": ([ctypes.POINTER(XentStruct), vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp],
+            "rsc_xent": ([ctypes.POINTER(XentStruct), vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp],
                          ctypes.c_int),
-            "rsc_xent_backward_workspace_bytes": ([ctypes.POINTER(XentStruct), i32, i32], sz),
+            "rsc_xent_backward_workspace_bytes": ([ctypes.POINTER(XentStruct), i32, i32, i32], sz),
             "rsc_xent_backward": ([ctypes.POINTER(XentStruct), vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64,
-                                   vp, vp, sz, vp], ctypes.c_int),
+                                   vp, i64, vp, vp, sz, vp], ctypes.c_int),
             "rsc_adamw_workspace_bytes": ([], sz),
             "rsc_adamw_step": ([ctypes.POINTER(AdamwStruct), vp, i32, vp, vp, sz, vp], ctypes.c_int),
             "rsc_adamw_moments": ([vp, i32, vp, vp, vp], ctypes.c_int),

@@ -90,6 +90,13 @@ rsc_status_t check_xent_operands(const rsc_xent_t *p, const void *X, int64_t ldx
     return RSC_OK;
 }
 
+rsc_status_t check_kept(const rsc_xent_t *p, const void *G, int64_t ldg) {
+    if (p->v > rsc::kKeptClasses || p->reduction == 0)
+        return fail(RSC_ERR_UNSUPPORTED, "G: %d classes (at most %d), reduction %d (1 or 2)", p->v, rsc::kKeptClasses,
+                    p->reduction);
+    return check_matrix(G, p->n, p->v, ldg, p->dtype, "G");
+}
+
 rsc::Classes classes_of(const rsc_xent_t *p, const void *bias, const void *targets) {
     rsc::Classes c;
     c.targets = targets;
@@ -197,29 +204,32 @@ size_t rsc_xent_workspace_bytes(const rsc_xent_t *p) {
 }
 
 rsc_status_t rsc_xent(const rsc_xent_t *p, const void *X, int64_t ldx, const void *W, int64_t ldw, const void *bias,
-                      const void *targets, float *loss, float *lse, float *count, void *ws, size_t ws_bytes,
-                      hipStream_t stream) {
+                      const void *targets, float *loss, float *lse, float *count, void *G, int64_t ldg, void *ws,
+                      size_t ws_bytes, hipStream_t stream) {
     RSC_TRY(check_xent(p));
     RSC_TRY(check_xent_operands(p, X, ldx, W, ldw, bias, targets));
     if (p->n > 0 || p->reduction != 0) RSC_TRY(check_scalar(loss, "loss"));
     if (p->n > 0) RSC_TRY(check_scalar(lse, "lse"));
     if (p->reduction != 0) RSC_TRY(check_scalar(count, "count"));
+    if (G) RSC_TRY(check_kept(p, G, ldg));
     RSC_TRY(check_ws(ws, ws_bytes, rsc_xent_workspace_bytes(p), "xent"));
     RSC_TRY(check_device());
-    RSC_HIP(rsc::loss_launch(loss_of(p), X, ldx, W, ldw, classes_of(p, bias, targets), loss, lse, count, ws, stream),
-            "xent launch");
+    rsc::Classes c = classes_of(p, bias, targets);
+    c.grad = G;
+    c.ldgrad = ldg;
+    RSC_HIP(rsc::loss_launch(loss_of(p), X, ldx, W, ldw, c, loss, lse, count, ws, stream), "xent launch");
     return RSC_OK;
 }
 
-size_t rsc_xent_backward_workspace_bytes(const rsc_xent_t *p, int32_t with_dx, int32_t with_dw) {
+size_t rsc_xent_backward_workspace_bytes(const rsc_xent_t *p, int32_t with_dx, int32_t with_dw, int32_t with_g) {
     if (check_xent(p) != RSC_OK) return 0;
-    return rsc::loss_backward_ws_bytes(loss_of(p), with_dx != 0, with_dw != 0);
+    return rsc::loss_backward_ws_bytes(loss_of(p), with_dx != 0, with_dw != 0, with_g != 0);
 }
 
 rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const void *X, int64_t ldx, const void *W,
                                int64_t ldw, const void *bias, const void *targets, const float *lse,
-                               const float *count, void *dX, int64_t lddx, void *dW, int64_t lddw, void *dbias,
-                               void *ws, size_t ws_bytes, hipStream_t stream) {
+                               const float *count, const void *G, int64_t ldg, void *dX, int64_t lddx, void *dW,
+                               int64_t lddw, void *dbias, void *ws, size_t ws_bytes, hipStream_t stream) {
     RSC_TRY(check_xent(p));
     RSC_TRY(check_xent_operands(p, X, ldx, W, ldw, bias, targets));
     if (p->n > 0 || p->reduction != 0) RSC_TRY(check_scalar(dloss, "dloss"));
@@ -229,7 +239,9 @@ rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const vo
     if (dW)
         RSC_TRY(check_matrix(dW, p->w_out_major ? p->v : p->k, p->w_out_major ? p->k : p->v, lddw, p->dtype, "dW"));
     RSC_TRY(check_vector(dbias, p->bias_dtype, p->dtype, "dbias"));
-    RSC_TRY(check_ws(ws, ws_bytes, rsc_xent_backward_workspace_bytes(p, dX != nullptr, dW != nullptr),
+    if (G) RSC_TRY(check_kept(p, G, ldg));
+    RSC_TRY(check_ws(ws, ws_bytes,
+                     rsc_xent_backward_workspace_bytes(p, dX != nullptr, dW != nullptr, G != nullptr),
                      "xent backward"));
     RSC_TRY(check_device());
     rsc::LossGrads g;
@@ -241,7 +253,9 @@ rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const vo
     g.db_f32 = p->bias_dtype == RSC_F32;
     rsc::Classes c = classes_of(p, bias, targets);
     c.lse = lse;
-    RSC_HIP(rsc::loss_backward_launch(loss_of(p), dloss, X, ldx, W, ldw, c, count, g, ws, stream),
+    c.grad = const_cast<void *>(G);  // (read only)
+    c.ldgrad = ldg;
+    RSC_HIP(rsc::loss_backward_launch(loss_of(p), dloss, X, ldx, W, ldw, c, count, g, G != nullptr, ws, stream),
             "xent backward launch");
     return RSC_OK;
 }

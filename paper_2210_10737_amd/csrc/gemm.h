@@ -824,6 +824,37 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
         for (int w = 0; w < WN; ++w) s += sum[w * BM + row] * expf(top[w * BM + row] - base);
         c.stats[(int64_t)o.n * p.m + m] = make_float2(mx, s);
     }
+    if (!c.grad) return;
+    // All classes are in this tile (the caller's one condition for c.grad): the
+    // logits' gradient for weight 1 leaves with them
+#pragma unroll
+    for (int i = 0; i < G::TA; ++i) {
+        const int row = (wm * G::TA + i) * 32 + (lane & 31), m = o.m * BM + row;
+        float mx = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int w = 0; w < WN; ++w) mx = fmaxf(mx, top[w * BM + row]);
+        const float base = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int w = 0; w < WN; ++w) s += sum[w * BM + row] * expf(top[w * BM + row] - base);
+        const float lse = mx + logf(s);
+        const int64_t t = m < p.m ? c.target(m) : -1;
+        const bool left_out = m >= p.m || c.left_out(m), bad = !left_out && (t < 0 || t >= p.n);
+#pragma unroll
+        for (int j = 0; j < G::TB; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int n = n0 + j * 32 + 8 * (r >> 2) + (r & 3);
+                const float g = c.scale * (exp_of<T>(acc[i][j][r] - lse) - (n == t ? 1.f : 0.f));
+                acc[i][j][r] = left_out ? 0.f : bad ? NAN : g;
+            }
+    }
+    __syncthreads();  // top and sum are read out
+    constexpr int W = kWidth<T>;
+    const Spot at = spot_of<G, W>(p, o.m * BM, o.n * BN);
+    by_rows<G, W>(acc, lds, [&](int down, float (&v)[W]) {
+        if (at.count > 0 && at.m + down < p.m)
+            store_row((T *)c.grad + (at.m * c.ldgrad + at.n) + down * c.ldgrad, at.count, v);
+    });
 }
 
 // The logits' gradient over one piece of the classes, from recomputed logits:

@@ -52,7 +52,9 @@ hipError_t RSC_CAT(product_, RSC_NAME)(int shape, const Product &p, const Epilog
         gemm::product_kernel<RSC_T, RSC_AC, RSC_BC, C><<<blocks_of(p, C::BM, C::BN), C::THREADS, 0, stream>>>(p, e);
         if (p.splits > 1) {
             const int64_t threads = p.m * ceil_div(p.n, gemm::kWidth<RSC_T>);
-            if (threads < 32768 && p.splits > 4)
+            if (threads < 8192 && p.splits > 32)
+                gemm::join_kernel<RSC_T, 32><<<(unsigned)ceil_div(threads * 32, 256), 256, 0, stream>>>(p, e);
+            else if (threads < 32768 && p.splits > 4)
                 gemm::join_kernel<RSC_T, 8><<<(unsigned)ceil_div(threads * 8, 256), 256, 0, stream>>>(p, e);
             else
                 gemm::join_kernel<RSC_T, 1><<<(unsigned)ceil_div(threads, 256), 256, 0, stream>>>(p, e);

@@ -53,18 +53,19 @@ struct Classes {
     // stats[j * rows + m]; the logit of the row's own class
     float2 *stats = nullptr;
     float *own_logit = nullptr;
-    // gradient pass
+    // gradient pass, and the statistics pass where it leaves the gradient too
     const float *lse = nullptr, *weight = nullptr;
     float scale = 1.f;
     int64_t first = 0;  // the piece's first class
     void *grad = nullptr;
     int64_t ldgrad = 0;
 
-    // the row's class; -1 for a row that is left out
-    __device__ __forceinline__ int64_t target(int m) const {
-        const int64_t t = targets_i32 ? (int64_t)((const int32_t *)targets)[m] : ((const int64_t *)targets)[m];
-        return t == ignore ? -1 : t;
+    __device__ __forceinline__ int64_t raw(int m) const {
+        return targets_i32 ? (int64_t)((const int32_t *)targets)[m] : ((const int64_t *)targets)[m];
     }
+    __device__ __forceinline__ bool left_out(int m) const { return raw(m) == ignore; }
+    // the row's class; -1 for a row that is left out
+    __device__ __forceinline__ int64_t target(int m) const { return left_out(m) ? -1 : raw(m); }
 };
 
 // ---- products (gemm_*.hip) ----------------------------------------------------
@@ -132,8 +133,12 @@ hipError_t column_sum_launch(int32_t dtype, const void *a, int64_t lda, int64_t 
 struct Loss {
     int32_t dtype, n, k, v, out_major, reduction;  // reduction: 0 none, 1 sum, 2 mean
 };
+// up to this many classes the statistics pass can leave the logits' gradient
+// (they are one tile of every shape)
+constexpr int kKeptClasses = 64;
 size_t loss_ws_bytes(const Loss &l);
-size_t loss_backward_ws_bytes(const Loss &l, bool dx, bool dw);
+// kept: the gradient that the statistics pass left is given
+size_t loss_backward_ws_bytes(const Loss &l, bool dx, bool dw, bool kept);
 hipError_t loss_launch(const Loss &l, const void *x, int64_t ldx, const void *w, int64_t ldw, const Classes &c,
                        float *loss, float *lse, float *count, void *ws, hipStream_t stream);
 struct LossGrads {
@@ -142,7 +147,7 @@ struct LossGrads {
     int32_t db_f32 = 0;
 };
 hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x, int64_t ldx, const void *w,
-                                int64_t ldw, Classes c, const float *count, const LossGrads &g, void *ws,
-                                hipStream_t stream);
+                                int64_t ldw, Classes c, const float *count, const LossGrads &g, bool kept,
+                                void *ws, hipStream_t stream);
 
 }  // namespace rsc

@@ -221,7 +221,11 @@ def _xent_struct(x, weight, out_major, targets, b_dtype, ignore_index, reduction
                       int(targets.dtype == torch.int32), b_dtype, ignore_index)
 
 
-def _xent_forward(x, weight, targets, bias, ignore_index: int, reduction: int):
+_KEPT_CLASSES = 64   # rsc_xent's bound for leaving the logits' gradient
+
+
+def _xent_forward(x, weight, targets, bias, ignore_index: int, reduction: int, keep: bool = False):
+    """(loss, lse and divisor, the logits' gradient or None, the aligned x and weight)."""
     n, dev = x.shape[0], x.device
     xa, ldx = _matrix(x)
     wa, ldw, out_major = _weights(weight)
@@ -230,25 +234,28 @@ def _xent_forward(x, weight, targets, bias, ignore_index: int, reduction: int):
     loss = torch.empty((n,) if reduction == 0 else (), dtype=torch.float32, device=dev)
     # lse of each row, behind it the divisor
     kept = torch.empty(n + 1, dtype=torch.float32, device=dev)
+    grad = _new(n, p.v, x.dtype, dev) if keep and p.v <= _KEPT_CLASSES and reduction != 0 else None
     need = lib().rsc_xent_workspace_bytes(ctypes.byref(p))
     ws = _workspace(need, dev)
     _check(lib().rsc_xent(ctypes.byref(p), xa.data_ptr(), ldx, wa.data_ptr(), ldw, pb, targets.data_ptr(),
-                          loss.data_ptr(), kept.data_ptr(), kept.data_ptr() + 4 * n, ws.data_ptr(), need, _stream()))
-    return loss, kept, xa, wa
+                          loss.data_ptr(), kept.data_ptr(), kept.data_ptr() + 4 * n,
+                          None if grad is None else grad.data_ptr(), 0 if grad is None else _ld(grad), ws.data_ptr(),
+                          need, _stream()))
+    return loss, kept, grad, xa, wa
 
 
 class _Xent(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, targets, bias, ignore_index, reduction):
-        loss, kept, xa, wa = _xent_forward(x, weight, targets, bias, ignore_index, reduction)
-        ctx.save_for_backward(xa, wa, targets, bias, kept)
+        loss, kept, grad, xa, wa = _xent_forward(x, weight, targets, bias, ignore_index, reduction, True)
+        ctx.save_for_backward(xa, wa, targets, bias, kept, grad)
         ctx.options = (ignore_index, reduction)
         return loss
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dloss):
-        x, weight, targets, bias, kept = ctx.saved_tensors
+        x, weight, targets, bias, kept, grad = ctx.saved_tensors
         ignore_index, reduction = ctx.options
         need_x, need_w, _, need_b = ctx.needs_input_grad[:4]
         n, dev, dtype = x.shape[0], x.device, x.dtype
@@ -261,10 +268,11 @@ class _Xent(torch.autograd.Function):
         dx = _new(n, weight.shape[0], dtype, dev) if need_x else None
         dw, lddw = _new_like_weights(weight, out_major) if need_w else (None, 0)
         db = torch.empty(weight.shape[1], dtype=bias.dtype, device=dev) if need_b else None
-        need = lib().rsc_xent_backward_workspace_bytes(ctypes.byref(p), need_x, need_w)
+        need = lib().rsc_xent_backward_workspace_bytes(ctypes.byref(p), need_x, need_w, grad is not None)
         ws = _workspace(need, dev)
         _check(lib().rsc_xent_backward(ctypes.byref(p), dloss.data_ptr(), x.data_ptr(), ldx, weight.data_ptr(), ldw,
                                        pb, targets.data_ptr(), kept.data_ptr(), kept.data_ptr() + 4 * n,
+                                       None if grad is None else grad.data_ptr(), 0 if grad is None else _ld(grad),
                                        None if dx is None else dx.data_ptr(), 0 if dx is None else _ld(dx),
                                        None if dw is None else dw.data_ptr(), lddw,
                                        None if db is None else db.data_ptr(), ws.data_ptr(), need, _stream()))
@@ -281,7 +289,8 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.T
     targets int64 or int32 [n]. Rows of ignore_index count for nothing; any
     other target outside 0 .. v-1 gives NaN. reduction: mean over the rows that
     count (0 if there is none), sum, or none (a loss per row). Differentiable
-    once in x, weight and bias; the logits are then formed again."""
+    once in x, weight and bias: the logits are then formed again, except that
+    up to 64 classes the forward pass keeps their gradient (n x v values)."""
     if reduction not in _REDUCTIONS:
         raise ValueError(f"reduction {reduction!r}: none, sum or mean expected")
     if targets.dtype not in (torch.int64, torch.int32):

@@ -76,9 +76,10 @@ def loss(dtype=0, n=10, k=20, v=12, out_major=0, reduction=2, i32=0, bias_dtype=
 
 def test_xent_refusals():
     def call(p=None, X=0x1000, ldx=32, W=0x2000, ldw=16, bias=None, t=0x3000, out=0x4000, lse=0x5000, count=0x6000,
-             ws=WS, ws_bytes=1 << 30):
+             ws=WS, ws_bytes=1 << 30, G=None, ldg=16):
         p = loss() if p is None else p
-        return name(rsc.lib().rsc_xent(ctypes.byref(p), X, ldx, W, ldw, bias, t, out, lse, count, ws, ws_bytes, None))
+        return name(rsc.lib().rsc_xent(ctypes.byref(p), X, ldx, W, ldw, bias, t, out, lse, count, G, ldg, ws, ws_bytes,
+                                       None))
 
     for bad in (dict(dtype=3), dict(n=-1), dict(k=0), dict(v=0), dict(reduction=3), dict(reduction=-1)):
         assert call(loss(**bad)) == BAD, bad
@@ -87,20 +88,23 @@ def test_xent_refusals():
     assert call(t=0x3004) == UNSUPPORTED and call(t=0x3002, p=loss(i32=1)) == UNSUPPORTED
     assert call(out=0x4002) == UNSUPPORTED and call(ldx=22) == UNSUPPORTED and call(ldw=8) == BAD
     assert call(loss(bias_dtype=1), bias=0x7000) == BAD
+    assert call(loss(v=65), ldw=68, G=0x8000, ldg=68) == UNSUPPORTED and call(loss(reduction=0), G=0x8000) == UNSUPPORTED
+    assert call(G=0x8004) == UNSUPPORTED and call(G=0x8000, ldg=8) == BAD
     need = rsc.lib().rsc_xent_workspace_bytes(ctypes.byref(loss()))
     assert call(ws_bytes=need - 1) == CAPACITY and call(ws=None) == BAD and call(ws=WS + 8) == UNSUPPORTED
 
     def back(p=None, d=0x9000, X=0x1000, W=0x2000, t=0x3000, lse=0x5000, count=0x6000, dX=0xa000, lddx=32, dW=0xb000,
-             lddw=16, db=None, ws=WS, ws_bytes=1 << 30):
+             lddw=16, db=None, ws=WS, ws_bytes=1 << 30, G=None, ldg=16):
         p = loss() if p is None else p
-        return name(rsc.lib().rsc_xent_backward(ctypes.byref(p), d, X, 32, W, 16, None, t, lse, count, dX, lddx, dW,
-                                                lddw, db, ws, ws_bytes, None))
+        return name(rsc.lib().rsc_xent_backward(ctypes.byref(p), d, X, 32, W, 16, None, t, lse, count, G, ldg, dX, lddx,
+                                                dW, lddw, db, ws, ws_bytes, None))
 
     for null in ("d", "X", "W", "t", "lse", "count"):
         assert back(**{null: None}) == BAD, null
     assert back(lddx=16) == BAD and back(dW=0xb004) == UNSUPPORTED
-    need = rsc.lib().rsc_xent_backward_workspace_bytes(ctypes.byref(loss()), 1, 1)
+    need = rsc.lib().rsc_xent_backward_workspace_bytes(ctypes.byref(loss()), 1, 1, 0)
     assert back(ws_bytes=need - 1) == CAPACITY
+    assert back(loss(reduction=0), G=0x8000) == UNSUPPORTED and back(G=0x8000, ldg=13) == UNSUPPORTED
 
 
 def tensor(param=0x1000, grad=0x2000, m=0x3000, v=0x4000, master=None, ms=None, vs=None, n=100):
@@ -145,8 +149,8 @@ def test_workspaces_hold_any_documented_size():
                     for flags in ((0, 0, 1), (0, 1, 0), (1, 0, 0)):
                         assert L.rsc_linear_backward_workspace_bytes(ctypes.byref(p), *flags) <= all_of < 1 << 42
                     q = loss(dtype=dtype, n=n, k=k, v=m, out_major=out_major)
-                    some = L.rsc_xent_backward_workspace_bytes(ctypes.byref(q), 0, 1)
-                    assert 0 < some <= L.rsc_xent_backward_workspace_bytes(ctypes.byref(q), 1, 1) < 1 << 42
+                    some = L.rsc_xent_backward_workspace_bytes(ctypes.byref(q), 0, 1, 0)
+                    assert 0 < some <= L.rsc_xent_backward_workspace_bytes(ctypes.byref(q), 1, 1, 0) < 1 << 42
                     assert 0 < L.rsc_xent_workspace_bytes(ctypes.byref(q)) < 1 << 42
 
 
