@@ -518,8 +518,8 @@ rsc_status_t rsc_greedy_allocate_profiles(int32_t L, int32_t n, int64_t nnz, int
  *     captured into a HIP graph, whose replays read and write the same
  *     buffers and hold the scalar arguments of the capture. Results are
  *     bitwise reproducible.
- *   - Sizes must keep the number of 32 x 64 tiles of every product below 2^30
- *     (RSC_ERR_UNSUPPORTED). */
+ *   - The results of every product (n x m, n x k and k x m, either way round)
+ *     must be at most 2^24 tiles of 32 x 64 (RSC_ERR_UNSUPPORTED). */
 typedef enum { RSC_F32 = 0, RSC_BF16 = 1, RSC_F16 = 2 } rsc_dtype_t;
 typedef enum { RSC_ACT_NONE = 0, RSC_ACT_RELU = 1, RSC_ACT_GELU = 2, RSC_ACT_SILU = 3 } rsc_act_t;
 
@@ -608,7 +608,7 @@ rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const vo
  *   p = p (1 - lr weight_decay)
  *       - (m lr / (1 - beta1^t)) / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * in fp32, every operation rounded by itself. Tensors are contiguous, n
- * values each (0 allowed), and must not overlap one another.
+ * values each (0 allowed, below 2^34), and must not overlap one another.
  *   param, grad: `dtype`. master (nullable): fp32 values that the step is
  *   applied to; param then receives their rounding.
  *   state_bits 32: exp_avg, exp_avg_sq are fp32 (m, v).
@@ -619,8 +619,9 @@ rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const vo
  *   number t 2^40 + base + i + 1 of SplitMix64 seeded with `seed` (base: the
  *   preceding tensors' sizes, each rounded up to 256); sqrt(v) > 0 keeps a
  *   code of at least 1. A NaN gradient makes its block NaN.
- *   step: device, int64; incremented by the call, so a captured call advances
- *   with each replay. lr and the other options are those of the capture.
+ *   step: device, int64, the steps until now (0 .. 2^40 - 2); incremented by
+ *   the call, so a captured call advances with each replay. Its contents while
+ *   the call runs are unspecified. lr and the other options are those of the capture.
  * The descriptors are read on the host before the call returns. Workspace:
  * rsc_adamw_workspace_bytes(). */
 typedef struct {

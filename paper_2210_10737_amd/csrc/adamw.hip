@@ -348,7 +348,7 @@ hipError_t in_batches(const rsc_adamw_tensor_t *t, int32_t count, F f) {
         const rsc_adamw_tensor_t &x = t[i];
         if (x.n == 0) continue;
         const int64_t need = ceil_div(x.n, kChunk);
-        if (b.count == kTensors || blocks + need > (int64_t(1) << 30)) flush();
+        if (b.count == kTensors || blocks + need > (int64_t(1) << 23)) flush();  // 2^31 threads a launch
         blocks += need;
         static_cast<rsc_adamw_tensor_t &>(b.t[b.count]) = x;
         // 16-bit parameters and codes move by 8 and 4 bytes, which 16 covers

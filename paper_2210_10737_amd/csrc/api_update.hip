@@ -40,8 +40,10 @@ rsc_status_t check_vector(const void *p, int32_t vec_dtype, int32_t dtype, const
     return RSC_OK;
 }
 
+// Every shape's thread blocks then stay within 2^31 threads a launch, and row
+// numbers, with the last tile's, within int32.
 rsc_status_t check_tiles(int64_t a, int64_t b, const char *what) {
-    if (rsc::ceil_div(a, 32) * rsc::ceil_div(b, 64) >= (int64_t(1) << 30))
+    if (rsc::ceil_div(a, 32) * rsc::ceil_div(b, 64) > (int64_t(1) << 24))
         return fail(RSC_ERR_UNSUPPORTED, "%s: a product of %lld x %lld", what, (long long)a, (long long)b);
     return RSC_OK;
 }
@@ -115,7 +117,7 @@ rsc_status_t check_scalar(const void *p, const char *name) {
 
 rsc_status_t check_moments(const rsc_adamw_tensor_t &t, int32_t i, bool codes) {
     if (t.n < 0) return fail(RSC_ERR_INVALID_ARGUMENT, "tensor %d: n = %lld < 0", i, (long long)t.n);
-    if (t.n >= int64_t(1) << 40) return fail(RSC_ERR_UNSUPPORTED, "tensor %d: n = %lld", i, (long long)t.n);
+    if (t.n >= int64_t(1) << 34) return fail(RSC_ERR_UNSUPPORTED, "tensor %d: n = %lld", i, (long long)t.n);
     if (t.n == 0) return RSC_OK;
     if (!t.exp_avg || !t.exp_avg_sq || (codes && (!t.exp_avg_scale || !t.exp_avg_sq_scale)))
         return fail(RSC_ERR_INVALID_ARGUMENT, "tensor %d: a moment or its scale is NULL", i);

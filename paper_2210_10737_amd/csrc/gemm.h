@@ -411,8 +411,9 @@ struct Tile {
 };
 
 // the block's tile and range of k: neighbouring tiles go to one XCD (blocks
-// are dealt to the 8 XCDs in turn), eight rows of tiles after another, so that
-// the tiles in work at one time on an XCD share their operands in its L2
+// are dealt to the 8 XCDs in turn), four rows of tiles after another, so that
+// the 32 tiles in work at one time on an XCD, four by eight, share their
+// operands in its L2 (16384 x 4096 x 8192 bf16: 918 us, 960 with eight rows, 990 with 16)
 struct Place {
     int m, n, split;
 };
@@ -423,10 +424,10 @@ __device__ __forceinline__ Place place(int tiles_m, int tiles_n, int splits) {
     Place o;
     o.split = at / tiles;
     const int t = at - o.split * tiles;
-    const int per = 8 * tiles_n, g = t / per, in = t - g * per;
-    const int rows = min(8, tiles_m - g * 8);
+    const int per = 4 * tiles_n, g = t / per, in = t - g * per;
+    const int rows = min(4, tiles_m - g * 4);
     o.n = in / rows;
-    o.m = g * 8 + (in - o.n * rows);
+    o.m = g * 4 + (in - o.n * rows);
     return o;
 }
 

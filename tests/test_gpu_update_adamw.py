@@ -316,3 +316,22 @@ def test_refusals():
     for bad in (dict(state_bits=16), dict(betas=(0.9, 1.0)), dict(lr=-1.0)):
         with pytest.raises(ValueError):
             rsc.AdamW([p], **bad)
+
+
+def test_more_than_2_to_31_elements():
+    """The last values of a tensor of more than 2^31 elements, 8-bit moments."""
+    n = 2 ** 31 + 1000
+    first = 2 ** 31    # a whole number of blocks
+    p = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    g = torch.full((n,), 0.01, dtype=torch.bfloat16, device="cuda")
+    g[first:] = torch.linspace(-1, 1, n - first, device="cuda").to(torch.bfloat16)
+    m, v = torch.full((n,), 20, dtype=torch.int8, device="cuda"), torch.full((n,), 30, dtype=torch.uint8, device="cuda")
+    ms, vs = (torch.full(((n + 255) // 256,), s, device="cuda") for s in (0.01, 0.02))
+    step = torch.full((1,), 3, dtype=torch.int64, device="cuda")
+    want = step_host(host(p[first:]), host(g[first:]), host(m[first:]), host(v[first:]), host(ms[first // 256:]),
+                     host(vs[first // 256:]), 4, first, 7, OPTS["lr"], OPTS["betas"], OPTS["eps"], OPTS["weight_decay"])
+    rsc.adamw_step([p], [g], [m], [v], step, exp_avg_scales=[ms], exp_avg_sq_scales=[vs], seed=7, **OPTS)
+    assert torch.equal(p[first:].cpu(), torch.from_numpy(want[0]).to(torch.bfloat16))
+    assert same(host(m[first:]), want[1]) and same(host(v[first:]), want[2])
+    assert same(host(ms[first // 256:]), want[3]) and same(host(vs[first // 256:]), want[4])
+    assert int(step) == 4

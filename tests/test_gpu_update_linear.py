@@ -279,3 +279,37 @@ def test_refusals():
     gx, = torch.autograd.grad(y.sum(), xg, create_graph=True)
     with pytest.raises(RuntimeError):
         torch.autograd.grad(gx.sum(), xg)
+
+
+def test_offsets_past_32_bits():
+    """An operand of 4.5 GB: its last rows, and the sum over all of them."""
+    n, k, m = 2_200_003, 1024, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty((n, k), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, n, 200_000):
+        part = x[i:i + 200_000]
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda"))
+    w = rand((k, m), torch.bfloat16, g, 1 / 32).requires_grad_()
+    y = rsc.linear(x, w)
+    dy = rand((n, m), torch.bfloat16, g)
+    dw, = torch.autograd.grad(y, w, dy)
+    w6 = w.detach().double()
+    for a in (0, n // 2, n - 300):
+        xs = x[a:a + 300].double()
+        want = xs @ w6
+        close(y.detach()[a:a + 300], want, sums(k) * (xs.abs() @ w6.abs()) + half(torch.bfloat16) * want.abs(), a)
+    want, mag = (torch.zeros((k, m), dtype=torch.float64, device="cuda") for _ in range(2))
+    for i in range(0, n, 100_000):
+        xs, ds = x[i:i + 100_000].double(), dy[i:i + 100_000].double()
+        want += xs.t() @ ds
+        mag += xs.abs().t() @ ds.abs()
+    # a split's chain of additions is at most n long
+    close(dw, want, sums(n) * mag + half(torch.bfloat16) * want.abs(), "dw")
+    # against weights of 4.5 GB, a column for each of their rows
+    wide = x[:2_200_000].view(275_000, 8192).t()
+    for rows, form in ((2, "few rows"), (40, "tiles")):
+        a = rand((rows, 8192), torch.bfloat16, g)
+        last = wide[:, -100:].double()
+        want = a.double() @ last
+        close(rsc.linear(a, wide)[:, -100:], want, sums(8192) * (a.double().abs() @ last.abs())
+              + half(torch.bfloat16) * want.abs(), form)

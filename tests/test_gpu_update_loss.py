@@ -79,9 +79,10 @@ def reference(x, w, b, t, ignore, reduction, up):
     return rows, rows_bound, weight[:, None] * p, weight.abs()[:, None] * off, weight.abs()[:, None] * p.abs(), count
 
 
-def check(n, k, v, dtype, out_major, bias, valid, reduction="mean", ignore=-100, i32=False, seed=5, up_scale=1.0):
+def check(n, k, v, dtype, out_major, bias, valid, reduction="mean", ignore=-100, i32=False, seed=5, up_scale=1.0,
+          bias_f32=False):
     x, w, b, t = inputs(n, k, v, dtype, out_major, valid, seed + n + 7 * k + 31 * v, ignore, i32)
-    b = b if bias else None
+    b = (b.float() if bias_f32 else b) if bias else None
     leaves = [a for a in (x, w, b) if a is not None]
     for a in leaves:
         a.requires_grad_()
@@ -118,7 +119,8 @@ def check(n, k, v, dtype, out_major, bias, valid, reduction="mean", ignore=-100,
     close(got[1], want, off + half(dtype) * (want.abs() + off) + small, ("dw", n, k, v))
     if bias:
         want, off = grad.sum(0), grad_off.sum(0)
-        close(got[2], want, off + half(dtype) * (want.abs() + off) + small, ("db", n, k, v))
+        assert got[2].dtype == b.dtype
+        close(got[2], want, off + half(b.dtype) * (want.abs() + off) + small, ("db", n, k, v))
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -134,6 +136,9 @@ def test_loss_and_gradients(size, out_major, dtype):
 def test_reductions_and_masks(valid, reduction, dtype):
     check(70, 48, 300, dtype, True, bias=False, valid=valid, reduction=reduction, i32=True)
     check(41, 48, 90, dtype, False, bias=True, valid=valid, reduction=reduction, ignore=3)
+    check(150, 48, 41, dtype, False, bias=True, valid=valid, reduction=reduction, ignore=3, bias_f32=True)
+    check(150, 40, 64, dtype, True, bias=False, valid=valid, reduction=reduction)
+    check(150, 40, 65, dtype, True, bias=True, valid=valid, reduction=reduction, bias_f32=True)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -173,11 +178,15 @@ def test_large_logits_and_masked_classes():
     assert float(rsc.linear_cross_entropy(x.detach(), w, t, b, reduction="none")[1]) == float("inf")
 
 
-def test_targets_out_of_range_show():
-    x, w, b, t = inputs(20, 16, 30, torch.float32, True, 1.0, 2)
-    for bad in (30, -1, 1 << 40):
+@pytest.mark.parametrize("v", [30, 300])
+def test_targets_out_of_range_show(v):
+    x, w, b, t = inputs(20, 16, v, torch.float32, True, 1.0, 2)
+    for bad in (v, -1, 1 << 40):
         t2 = t.clone()
         t2[4] = bad
+        xg = x.clone().requires_grad_()
+        g, = torch.autograd.grad(rsc.linear_cross_entropy(xg, w, t2, b), xg)
+        assert bool(g[4].isnan().all()) and not g[:4].isnan().any() and not g[5:].isnan().any()
         rows = rsc.linear_cross_entropy(x, w, t2, b, reduction="none")
         assert bool(rows.isnan().nonzero()[:, 0].eq(4).all()) and int(rows.isnan().sum()) == 1
         assert bool(rsc.linear_cross_entropy(x, w, t2, b).isnan())
@@ -190,7 +199,7 @@ def test_no_rows(dtype):
     b = torch.ones(5, dtype=dtype, device="cuda", requires_grad=True)
     t = torch.empty(0, dtype=torch.int64, device="cuda")
     loss = rsc.linear_cross_entropy(x, w, t, b)
-    assert float(loss) == 0.0
+    assert float(loss.detach()) == 0.0
     gx, gw, gb = torch.autograd.grad(loss, [x, w, b])
     assert tuple(gx.shape) == (0, 12) and not gw.any() and not gb.any()
     assert tuple(rsc.linear_cross_entropy(x, w, t, b, reduction="none").shape) == (0,)

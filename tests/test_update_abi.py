@@ -45,6 +45,7 @@ def test_linear_refusals():
     assert forward(pre=0x4000) == BAD                     # pre is Y
     assert forward(Y=0x1000, ldy=32) == BAD               # Y is X
     assert forward(layer(n=1 << 30, m=1 << 18), ldy=1 << 18, ldw=1 << 18) == UNSUPPORTED   # too many tiles
+    assert forward(layer(n=2 ** 31 - 1)) == UNSUPPORTED
     big = layer(n=64, k=8192, m=64)
     need = rsc.lib().rsc_linear_workspace_bytes(ctypes.byref(big))
     assert need > 0                                       # few tiles, a long sum: split
@@ -123,7 +124,7 @@ def test_adamw_refusals():
                 dict(bits=8), dict(ws=None)):
         assert call(**bad) == BAD, bad
     for bad in (dict(step=0x8004), dict(t=tensor(param=0x1002)), dict(t=tensor(v=0x4001)), dict(t=tensor(master=0x1001)),
-                dict(t=tensor(n=1 << 40)), dict(bits=8, t=tensor(ms=0x5002, vs=0x6000)), dict(ws=WS + 4)):
+                dict(t=tensor(n=1 << 34)), dict(bits=8, t=tensor(ms=0x5002, vs=0x6000)), dict(ws=WS + 4)):
         assert call(**bad) == UNSUPPORTED, bad
     assert call(ws_bytes=255) == CAPACITY
     L = rsc.lib()
@@ -144,6 +145,9 @@ def test_workspaces_hold_any_documented_size():
         for n in (0, 1, 7, 300, 5000, 700000, 3000000):
             for k, m in ((1, 1), (64, 41), (300, 512), (4096, 4096), (1024, 131072)):
                 for out_major in (0, 1):
+                    if -(-n // 32) * -(-m // 64) > 1 << 24:
+                        assert L.rsc_linear_backward_workspace_bytes(ctypes.byref(layer(n=n, k=k, m=m)), 1, 1, 1) == 0
+                        continue
                     p = layer(dtype=dtype, act=1, n=n, k=k, m=m, out_major=out_major)
                     all_of = L.rsc_linear_backward_workspace_bytes(ctypes.byref(p), 1, 1, 1)
                     for flags in ((0, 0, 1), (0, 1, 0), (1, 0, 0)):
