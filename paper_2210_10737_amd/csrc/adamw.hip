@@ -120,14 +120,16 @@ __device__ __forceinline__ void get4(const T *p, int n, bool vec, T (&v)[COUNT])
         for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : (T)0;
     }
 }
-template <typename T, int COUNT>
+// STREAM: past the caches
+template <bool STREAM, typename T, int COUNT>
 __device__ __forceinline__ void put4(T *p, int n, bool vec, const T (&v)[COUNT]) {
     typedef T v4 __attribute__((ext_vector_type(4)));
     if (vec) {
         v4 x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = v[i];
-        *(v4 *)p = x;
+        if (STREAM) __builtin_nontemporal_store(x, (v4 *)p);
+        else *(v4 *)p = x;
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -257,12 +259,12 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, AdamwRates a, const 
                 r_bits = max(r_bits, __float_as_uint(r[i]) & 0x7fffffffu);
             }
         }
-        if (t.master) put4(t.master + at, f.n, f.vec, p);
+        if (t.master) put4<!ONE>(t.master + at, f.n, f.vec, p);
         {
             T y[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = (T)p[i];
-            put4((T *)t.param + at, f.n, f.vec, y);
+            put4<!ONE>((T *)t.param + at, f.n, f.vec, y);
         }
         if (CODES) {
             const float m_top = wave_max(__uint_as_float(m_bits)), r_top = wave_max(__uint_as_float(r_bits));
@@ -279,15 +281,15 @@ __global__ __launch_bounds__(256) void step_kernel(Batch b, AdamwRates a, const 
                 const float qr = encode(r[i], r_top, r_inv, 255.f, (uint32_t)((z >> 24) & 0xffffffu));
                 c[i] = (uint8_t)(r[i] > 0.f ? fmaxf(qr, 1.f) : qr);
             }
-            put4((int8_t *)t.exp_avg + at, f.n, f.vec, q);
-            put4((uint8_t *)t.exp_avg_sq + at, f.n, f.vec, c);
+            put4<!ONE>((int8_t *)t.exp_avg + at, f.n, f.vec, q);
+            put4<!ONE>((uint8_t *)t.exp_avg_sq + at, f.n, f.vec, c);
             if ((threadIdx.x & 63) == 0) {
                 t.exp_avg_scale[at >> 8] = m_top;
                 t.exp_avg_sq_scale[at >> 8] = r_top;
             }
         } else {
-            put4((float *)t.exp_avg + at, f.n, f.vec, m);
-            put4((float *)t.exp_avg_sq + at, f.n, f.vec, v);
+            put4<!ONE>((float *)t.exp_avg + at, f.n, f.vec, m);
+            put4<!ONE>((float *)t.exp_avg_sq + at, f.n, f.vec, v);
         }
     }
 }
@@ -324,8 +326,8 @@ __global__ __launch_bounds__(256) void moments_kernel(Batch b) {
             const float root = decode((float)c[k][i], (float)(1.0 / 255)) * rs[k];
             v[i] = root * root;
         }
-        put4(t.master + at, n, vec, m);
-        put4((float *)t.param + at, n, vec, v);
+        put4<true>(t.master + at, n, vec, m);
+        put4<true>((float *)t.param + at, n, vec, v);
     }
 }
 

@@ -180,7 +180,7 @@ StatsFn grad_fn(const Loss &l) {
     return f[l.dtype][l.out_major ? 1 : 0];
 }
 
-int rows_split(int64_t tiles) { return tiles >= 16 ? 16 : 1; }
+int rows_split(int64_t tiles) { return tiles >= 4 ? 16 : 1; }
 
 }  // namespace
 
