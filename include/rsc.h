@@ -527,13 +527,18 @@ typedef enum { RSC_ACT_NONE = 0, RSC_ACT_RELU = 1, RSC_ACT_GELU = 2, RSC_ACT_SIL
  *   X: n x k. R, Y: n x m. W: k x m, stored as k rows of m values
  *   (w_out_major = 0, ldw >= m) or as m rows of k values (w_out_major = 1,
  *   ldw >= k). n >= 0, k >= 1, m >= 1.
- *   act: none, max(z, 0), z Phi(z) (the exact GELU), z / (1 + exp(-z)). */
+ *   act: none, max(z, 0), z Phi(z) (the exact GELU), z / (1 + exp(-z)).
+ *   for_gradients: with ReLU, the sign of results next to zero, on which
+ *   gradients hang, is decided by sums in 64 bits (at most 32 in each group of
+ *   some thousand results), and a positive one does not round to 0; without
+ *   effect otherwise. */
 typedef struct {
     int32_t dtype; /* rsc_dtype_t of X, W, R, Y */
     int32_t act;   /* rsc_act_t */
     int32_t n, k, m;
     int32_t w_out_major;
     float alpha, beta;
+    int32_t for_gradients; /* Y will be given to rsc_linear_backward */
 } rsc_linear_t;
 
 /* rsc_linear: bias, R and pre may be NULL; pre (n x m) receives Z, which the

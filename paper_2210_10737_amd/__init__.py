@@ -107,7 +107,7 @@ class CsrStruct(ctypes.Structure):
 class LinearStruct(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("n", ctypes.c_int32), ("k", ctypes.c_int32),
                 ("m", ctypes.c_int32), ("w_out_major", ctypes.c_int32), ("alpha", ctypes.c_float),
-                ("beta", ctypes.c_float)]
+                ("beta", ctypes.c_float), ("for_gradients", ctypes.c_int32)]
 
 
 class XentStruct(ctypes.Structure):

@@ -67,7 +67,8 @@ rsc_status_t check_linear(const rsc_linear_t *p) {
 }
 
 rsc::Linear layer_of(const rsc_linear_t *p) {
-    return rsc::Linear{p->dtype, p->act, p->n, p->k, p->m, p->w_out_major != 0, p->alpha, p->beta};
+    return rsc::Linear{p->dtype, p->act, p->n, p->k, p->m, p->w_out_major != 0, p->alpha, p->beta,
+                       p->for_gradients != 0};
 }
 
 rsc_status_t check_xent(const rsc_xent_t *p) {

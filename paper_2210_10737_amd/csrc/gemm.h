@@ -448,7 +448,7 @@ __device__ __forceinline__ float exp_of(float x) {
 }
 
 template <typename T>
-__device__ __forceinline__ float bias_at(const void *bias, int f32, int n) {
+__device__ __forceinline__ float bias_at(const void *bias, int f32, int64_t n) {
     return f32 ? ((const float *)bias)[n] : Type<T>::get(((const T *)bias)[n]);
 }
 
@@ -502,6 +502,12 @@ __device__ __forceinline__ void store_f32(float *p, int count, const float (&v)[
     }
 }
 
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+
 // the bias of a lane's columns, 0 without one or past the end
 template <typename T>
 __device__ __forceinline__ void load_bias(const void *bias, int f32, int n, int count, float (&v)[kWidth<T>]) {
@@ -516,26 +522,136 @@ struct Spot {
     int m, n, count;
 };
 
-// y = act(alpha sum + bias + beta r)
-template <typename T, int ACT>
-__device__ __forceinline__ void finish(float (&v)[kWidth<T>], const float (&bias)[kWidth<T>], const Epilogue &e,
-                                       float alpha, const Spot &at, int down) {
+// z = alpha sum + bias + beta r; r: what the residual adds (0 without one)
+template <typename T>
+__device__ __forceinline__ void argument(float (&v)[kWidth<T>], const float (&bias)[kWidth<T>], const Epilogue &e,
+                                         float alpha, const Spot &at, int down, float (&r)[kWidth<T>]) {
     constexpr int W = kWidth<T>;
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = fmaf(alpha, v[i], bias[i]);
     if (e.r) {
-        float r[W];
         if (e.r_f32) load_f32((const float *)e.r + (at.m * e.ldr + at.n) + down * e.ldr, at.count, r);
         else load_row((const T *)e.r + (at.m * e.ldr + at.n) + down * e.ldr, at.count, r);
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] = fmaf(e.beta, r[i], v[i]);
     }
+}
+// see mend()
+template <typename T>
+__device__ __forceinline__ float above_zero(float y) {
+    constexpr float smallest = std::is_same_v<T, _Float16> ? 0x1p-24f : 0x1p-126f;
+    return y > 0.f && Type<T>::get(Type<T>::put(y)) == 0.f ? smallest : y;
+}
+
+// y = act(z)
+template <typename T, int ACT>
+__device__ __forceinline__ void leave(float (&v)[kWidth<T>], const Epilogue &e, const Spot &at, int down) {
+    constexpr int W = kWidth<T>;
     if (e.pre) store_row((T *)e.pre + (at.m * e.ldpre + at.n) + down * e.ldpre, at.count, v, e.stream);
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = act_of<ACT>(v[i]);
+    if (ACT == kRelu && e.sure) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = above_zero<T>(v[i]);
+    }
     if (e.y_f32) store_f32((float *)e.y + (at.m * e.ldy + at.n) + down * e.ldy, at.count, v);
     else store_row((T *)e.y + (at.m * e.ldy + at.n) + down * e.ldy, at.count, v, e.stream);
 }
+
+// ---- the sign of a ReLU's argument ------------------------------------------
+// A ReLU's gradient hangs on the sign of its argument. A sum in fp32 that comes
+// out next to zero may have the other sign, which takes in or leaves out a whole
+// term of every gradient: among 10 million results of 1,021 terms about one. For results
+// that a backward pass will read (e.sure) those few are formed again in 64
+// bits, and a positive one that its type would round to 0 stays at the type's
+// smallest value.
+// sum over k of A(m, k) B(k, n) in 64 bits (products of the operands' types are
+// exact there), by the whole wave; A stored by rows
+template <typename T>
+__device__ __forceinline__ double dot64(const Product &p, int b_cols, int m, int n) {
+    constexpr int W = kWidth<T>;
+    const int lane = threadIdx.x & 63;
+    const T *const a = (const T *)p.a + m * p.lda;
+    double sum = 0.0;
+    for (int k = lane * W; k < p.k; k += 64 * W) {
+        float x[W], y[W];
+        load_row(a + k, p.k - k, x);
+        if (b_cols) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) y[i] = k + i < p.k ? Type<T>::get(((const T *)p.b)[(k + i) * p.ldb + n]) : 0.f;
+        } else {
+            load_row((const T *)p.b + n * p.ldb + k, p.k - k, y);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) sum = fma((double)x[i], (double)y[i], sum);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+    return sum;
+}
+
+// how far a sum of k terms may be off beside the largest sum around it: a
+// random walk of roundings takes it 2^-24 sqrt(k / 16) of that, this is more
+// than ten times as far
+__device__ __forceinline__ float doubt_of(float largest, int k) { return largest * 0x1p-24f * (8.f + sqrtf((float)k)); }
+
+// Is an argument next to zero? `others`: the magnitudes added to the sum. A sum
+// of exactly 0 is taken as such (a row of zeros).
+__device__ __forceinline__ bool unsure(float z, float sum, float others, float doubt) {
+    return sum != 0.f && fabsf(z) < fmaf(others, 0x1p-22f, doubt);
+}
+// what one wave forms again at most: operands of few different values can cancel
+// everywhere, but then their sums are exact
+constexpr int kBudget = 32;
+
+// A place to form again, and the residual's value there: Y may lie on R, and is
+// written by then.
+struct Again {
+    uint32_t place;
+    float r;
+};
+// Row m, column n once more, by the whole wave.
+template <typename T>
+__device__ __forceinline__ void mend(const Product &p, const Epilogue &e, float alpha, int m, int n, float r) {
+    double s = (double)alpha * dot64<T>(p, e.b_cols, m, n);
+    if (e.bias) s += (double)bias_at<T>(e.bias, e.bias_f32, n);
+    if (e.r) s += (double)e.beta * (double)r;
+    if ((threadIdx.x & 63) != 0) return;
+    const float z = (float)s, y = above_zero<T>(fmaxf(z, 0.f));
+    if (e.pre) ((T *)e.pre)[m * e.ldpre + n] = Type<T>::put(z);
+    if (e.y_f32) ((float *)e.y)[m * e.ldy + n] = y;
+    else ((T *)e.y)[m * e.ldy + n] = Type<T>::put(y);
+}
+
+// A wave's list of unsure places, in LDS. They are formed again when the wave's
+// rows are done: the accumulators are free by then. (Within the rows' loop the
+// 256 x 256 kernel spilled, and every product took 4 to 15 times as long.)
+struct Unsure {
+    Again *list;
+    int count = 0;  // the same in all lanes
+    // all lanes call it
+    template <typename T>
+    __device__ __forceinline__ void note(const float (&z)[kWidth<T>], const float (&sum)[kWidth<T>],
+                                         const float (&bias)[kWidth<T>], const float (&r)[kWidth<T>],
+                                         const Epilogue &e, float doubt, uint32_t place, int width) {
+        constexpr int W = kWidth<T>;
+        uint32_t todo = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (i < width && unsure(z[i], sum[i], fabsf(bias[i]) + fabsf(e.beta * r[i]), doubt)) todo |= 1u << i;
+        while (const uint64_t who = __ballot(todo != 0)) {
+            const int at = count + __popcll(who & ((1ull << (threadIdx.x & 63)) - 1));
+            const int first = __ffs((int)todo) - 1;
+            float residual = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) residual = i == first ? r[i] : residual;
+            if (todo && at < kBudget) list[at] = Again{place + first, residual};
+            todo &= todo - 1;
+            count = min(count + __popcll(who), kBudget);
+        }
+    }
+};
+
 // f(the activation as a constant): one test a block
 template <typename F>
 __device__ __forceinline__ void with_act(int act, F f) {
@@ -628,11 +744,47 @@ __global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilo
     const Spot at = spot_of<G, W>(p, o.m * BM, o.n * BN);
     float bias[W];
     load_bias<T>(e.bias, e.bias_f32, at.n, at.count, bias);
+    const bool sure = !AC && e.act == kRelu && e.sure;  // (the forward pass)
+    float doubt = -1.f;  // (nothing is unsure)
+    if (sure) {
+        float largest = 0.f;
+#pragma unroll
+        for (int i = 0; i < G::TA; ++i)
+#pragma unroll
+            for (int j = 0; j < G::TB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(acc[i][j][r]));
+        doubt = doubt_of(fabsf(alpha) * wave_max(largest), p.k);
+    }
+    constexpr int SLABS = 32 * (G::TB * 32 + 4) * 4 * (C::THREADS / 64);
+    static_assert(SLABS + kBudget * (int)sizeof(Again) * (C::THREADS / 64) <= G::LDS, "the waves' rows and lists");
+    Unsure again{(Again *)(lds + SLABS) + kBudget * (threadIdx.x >> 6)};
     with_act(e.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
         by_rows<G, W>(acc, lds, [&](int down, float (&v)[W]) {
-            if (at.count > 0 && at.m + down < p.m) finish<T, decltype(act)::value>(v, bias, e, alpha, at, down);
+            const bool live = at.count > 0 && at.m + down < p.m;
+            if (ACT != kRelu && !live) return;
+            float sum[W], r[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                sum[i] = v[i];
+                r[i] = 0.f;
+            }
+            if (live) argument<T>(v, bias, e, alpha, at, down, r);
+            if (!AC && ACT == kRelu && sure)
+                again.note<T>(v, sum, bias, r, e, doubt, (uint32_t)(at.m + down - o.m * BM) << 16 | (at.n - o.n * BN),
+                              live ? at.count : 0);
+            if (live) leave<T, ACT>(v, e, at, down);
         });
     });
+    if (!AC && again.count > 0) {
+        // behind the rows' own stores
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        for (int i = 0; i < again.count; ++i) {
+            const Again x = again.list[i];
+            mend<T>(p, e, alpha, o.m * BM + (int)(x.place >> 16), o.n * BN + (int)(x.place & 0xffff), x.r);
+        }
+    }
 }
 
 // The sum of the splits' partial sums and the epilogue: L neighbouring threads
@@ -646,14 +798,14 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
     const int64_t ld = ld_partial(p.n), chunks = (p.n + W - 1) / W;
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
     const int part = threadIdx.x % L;
-    if (at >= chunks * p.m) return;
-    const int m = (int)(at / chunks), n = (int)(at % chunks) * W, count = p.n - n;
+    bool live = at < chunks * p.m;
+    const int m = live ? (int)(at / chunks) : 0, n = live ? (int)(at % chunks) * W : 0, count = p.n - n;
     const float *from = p.partial + m * ld + n;
     const int64_t step = (int64_t)p.m * ld;
     float v[W], bias[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = 0.f;
-    int s = part;
+    int s = live ? part : p.splits;
     for (; s + 3 * L < p.splits; s += 4 * L) {
         float x[4][W];
 #pragma unroll
@@ -673,10 +825,39 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
     for (int d = 1; d < L; d *= 2)
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] += __shfl_xor(v[i], d);
-    if (part != 0) return;
-    load_bias<T>(e.bias, e.bias_f32, n, count, bias);
+    live = live && part == 0;
+    const float alpha = alpha_of(e);
     const Spot spot{m, n, count};
-    with_act(e.act, [&](auto act) { finish<T, decltype(act)::value>(v, bias, e, alpha_of(e), spot, 0); });
+    float r[W], sum[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        sum[i] = v[i];
+        r[i] = bias[i] = 0.f;
+    }
+    if (live) {
+        load_bias<T>(e.bias, e.bias_f32, n, count, bias);
+        argument<T>(v, bias, e, alpha, spot, 0, r);
+    }
+    const bool sure = e.act == kRelu && e.sure;
+    __shared__ Again lists[4][kBudget];
+    Unsure again{lists[threadIdx.x >> 6]};
+    if (sure) {
+        float largest = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) largest = fmaxf(largest, fabsf(sum[i]));
+        const float doubt = doubt_of(fabsf(alpha) * wave_max(largest), p.k);
+        // places: the value's number among the wave's
+        again.note<T>(v, sum, bias, r, e, doubt, (threadIdx.x & 63) * W, live ? count : 0);
+    }
+    if (live) with_act(e.act, [&](auto act) { leave<T, decltype(act)::value>(v, e, spot, 0); });
+    if (again.count > 0) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        for (int i = 0; i < again.count; ++i) {
+            const Again x = again.list[i];
+            const int from = (int)x.place / W;
+            mend<T>(p, e, alpha, __shfl(m, from), __shfl(n, from) + (int)x.place % W, x.r);
+        }
+    }
 }
 
 // Few rows (R of them, 1 to kFewRows) against weights stored by rows: bound by
@@ -734,7 +915,9 @@ __global__ __launch_bounds__(256) void few_rows_kernel(Product p, Epilogue e) {
         }
     }
     // lane j R + r finishes column j of row r
+    const bool sure = e.act == kRelu && e.sure;
     float v = 0.f;
+    double exact = 0.0;
 #pragma unroll
     for (int j = 0; j < COLUMNS; ++j)
 #pragma unroll
@@ -742,16 +925,26 @@ __global__ __launch_bounds__(256) void few_rows_kernel(Product p, Epilogue e) {
 #pragma unroll
             for (int d = 32; d > 0; d /= 2) acc[j][r] += __shfl_xor(acc[j][r], d);
             if (lane == j * R + r) v = acc[j][r];
+            if (sure) {  // (the weights are in the caches now)
+                const double s = dot64<T>(p, 0, r, min(n0 + j, p.n - 1));
+                if (lane == j * R + r) exact = s;
+            }
         }
     const int n = n0 + lane / R, m = lane % R;
     if (lane >= COLUMNS * R || n >= p.n) return;
-    v = fmaf(alpha_of(e), v, e.bias ? bias_at<T>(e.bias, e.bias_f32, n) : 0.f);
+    const float alpha = alpha_of(e), bias = e.bias ? bias_at<T>(e.bias, e.bias_f32, n) : 0.f;
+    v = fmaf(alpha, v, bias);
+    exact = (double)alpha * exact + (double)bias;
     if (e.r) {
         const int64_t at = m * e.ldr + n;
-        v = fmaf(e.beta, e.r_f32 ? ((const float *)e.r)[at] : Type<T>::get(((const T *)e.r)[at]), v);
+        const float r = e.r_f32 ? ((const float *)e.r)[at] : Type<T>::get(((const T *)e.r)[at]);
+        v = fmaf(e.beta, r, v);
+        exact += (double)e.beta * (double)r;
     }
+    if (sure) v = (float)exact;
     if (e.pre) ((T *)e.pre)[m * e.ldpre + n] = Type<T>::put(v);
     with_act(e.act, [&](auto act) { v = act_of<decltype(act)::value>(v); });
+    if (sure) v = above_zero<T>(v);
     if (e.y_f32) ((float *)e.y)[m * e.ldy + n] = v;
     else ((T *)e.y)[m * e.ldy + n] = Type<T>::put(v);
 }

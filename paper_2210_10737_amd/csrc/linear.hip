@@ -330,6 +330,8 @@ hipError_t linear_launch(const Linear &l, const void *x, int64_t ldx, const void
     e.ldy = ldy;
     e.pre = pre;
     e.ldpre = ldpre;
+    e.sure = l.sure;
+    e.b_cols = !l.out_major;
     return product_launch(l.dtype, l.out_major ? kRowsRows : kRowsCols, p, e, ws, stream);
 }
 

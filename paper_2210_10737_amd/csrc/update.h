@@ -40,6 +40,9 @@ struct Epilogue {
     int64_t ldpre = 0;
     // results go past the caches (set by the launch for large ones)
     bool stream = false;
+    // ReLU: signs next to zero are decided in 64 bits; B's storage then
+    bool sure = false;
+    int32_t b_cols = 0;
 };
 
 // What the loss's products need besides X and W
@@ -109,6 +112,7 @@ inline size_t value_size(int32_t dtype) { return dtype == kF32 ? 4 : 2; }
 struct Linear {
     int32_t dtype, act, n, k, m, out_major;
     float alpha, beta;
+    bool sure;  // forward: Y is kept for the backward pass
 };
 size_t linear_ws_bytes(const Linear &l);
 size_t linear_backward_ws_bytes(const Linear &l, bool dx, bool dw, bool db);

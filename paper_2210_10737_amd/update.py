@@ -130,7 +130,7 @@ def _linear_forward(x, weight, bias, residual, act: int, alpha: float, beta: flo
     xa, ldx = _matrix(x)
     wa, ldw, out_major = _weights(weight)
     b, pb, b_dtype = _bias_arg(bias)
-    p = LinearStruct(_DTYPES[dtype], act, n, k, m, out_major, alpha, beta)
+    p = LinearStruct(_DTYPES[dtype], act, n, k, m, out_major, alpha, beta, keep)
     y = _new(n, m, dtype, dev) if out is None else out
     ra, ldr = (None, 0) if residual is None else _matrix(residual)
     pre = _new(n, m, dtype, dev) if keep and act >= 2 else None

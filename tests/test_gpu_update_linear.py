@@ -10,6 +10,7 @@ import pytest
 import torch
 
 import paper_2210_10737_amd as rsc
+from paper_2210_10737_amd import update
 
 pytestmark = pytest.mark.gpu
 
@@ -313,3 +314,46 @@ def test_offsets_past_32_bits():
         want = a.double() @ last
         close(rsc.linear(a, wide)[:, -100:], want, sums(8192) * (a.double().abs() @ last.abs())
               + half(torch.bfloat16) * want.abs(), form)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("out_major", [False, True])
+@pytest.mark.parametrize("size", [(5003, 1021, 1045), (900, 3001, 700), (64, 9000, 300), (2, 3000, 4000), (1, 700, 9000)])
+def test_relu_masks_are_those_of_64_bits(size, out_major, dtype):
+    """Every result of a pass that keeps gradients is above zero where the sum
+    in 64 bits is (of ten million random ones a few come out of fp32 sums with
+    the other sign, or round to 0 in fp16)."""
+    n, k, m = size
+    x, w, b, r, _ = inputs(n, k, m, dtype, out_major, 77)
+    for residual, beta in ((None, 1.0), (r, 0.5)):
+        y = rsc.linear(x.clone().requires_grad_(), w, b, residual=residual, act="relu", alpha=0.5, beta=beta)
+        z = 0.5 * (x.double() @ w.double()) + b.double() + (0 if residual is None else beta * residual.double())
+        assert torch.equal(y.detach() > 0, z > 0)
+
+
+def test_relu_masks_of_cancelled_sums():
+    """The residual takes all of the sum away but its rounding: 30 results that
+    32 bits cannot tell from zero. Rows of zeros and exact sums stay zero."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, w = rand((3, 50), torch.float32, g), rand((50, 10), torch.float32, g)
+    exact = x.double() @ w.double()
+    r = -exact.float()
+    y = rsc.linear(x.clone().requires_grad_(), w, residual=r, act="relu").detach()
+    z = exact + r.double()
+    assert torch.equal(y > 0, z > 0)
+    # one rounding to 32 bits, and on either side a 64-bit sum of 50 terms: up to
+    # 50 roundings of 2^-53 of the sum of magnitudes (here about 40: 2e-13)
+    sums64 = 2 * 50 * 2.0 ** -53 * (x.double().abs() @ w.double().abs())
+    assert bool(((y.double() - z.clamp_min(0)).abs() <= 2.0 ** -24 * z.abs() + sums64).all())
+    x, w = torch.zeros((500, 64), device="cuda"), rand((64, 300), torch.float32, g)
+    assert not rsc.linear(x.requires_grad_(), w, act="relu").any()
+    x = torch.randint(-1, 2, (500, 64), generator=g, device="cuda").float()
+    w = torch.randint(-1, 2, (64, 300), generator=g, device="cuda").float()
+    assert torch.equal(rsc.linear(x.clone().requires_grad_(), w, act="relu").detach(), torch.relu((x.double() @ w.double()).float()))
+    # results that lie on the residual
+    for size in ((700, 1021, 300), (64, 9000, 300), (2, 300, 400)):   # tiles, a split k, few rows
+        x, w, b, r, _ = inputs(*size, torch.float32, False, 5)
+        r = (-(x.double() @ w.double()) - b.double()).float().contiguous()
+        want = rsc.linear(x.clone().requires_grad_(), w, b, residual=r, act="relu").detach()
+        y, _, _, _ = update._linear_forward(x, w, b, r, 1, 1.0, 1.0, r, True)
+        assert y is r and torch.equal(y, want), size
