@@ -440,12 +440,18 @@ __device__ __forceinline__ float act_of(float z) {
     return z;
 }
 
-// exp of a difference of logits: to the rounding of fp32 where the result is
-// fp32, the hardware's (2 ulp and the argument's rounding) for 16-bit results
+// exp(v - base), for many v of one base. For fp32 results to the rounding of
+// fp32; for 16-bit ones by the hardware's power of two (2 ulp), with
+// base log2(e) rounded once: all of a base's results are off by the same factor
+// of at most 1 + |base| 2^-24.
 template <typename T>
-__device__ __forceinline__ float exp_of(float x) {
-    return sizeof(T) == 4 ? expf(x) : __expf(x);
-}
+struct ExpBelow {
+    float base;
+    __device__ __forceinline__ explicit ExpBelow(float b) : base(sizeof(T) == 4 ? b : b * 1.44269504089f) {}
+    __device__ __forceinline__ float operator()(float v) const {
+        return sizeof(T) == 4 ? expf(v - base) : __builtin_amdgcn_exp2f(fmaf(v, 1.44269504089f, -base));
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ float bias_at(const void *bias, int f32, int64_t n) {
@@ -522,25 +528,56 @@ struct Spot {
     int m, n, count;
 };
 
-// z = alpha sum + bias + beta r; r: what the residual adds (0 without one)
+// What the residual adds to a lane's columns, as read: fp32, or the operands' type
+// in x[0].
+template <int W>
+struct Rest {
+    v4f x[W / 4];
+};
+template <typename T>
+__device__ __forceinline__ Rest<kWidth<T>> fetch_rest(const Epilogue &e, const Spot &at, int down) {
+    constexpr int W = kWidth<T>;
+    Rest<W> g = {};
+    if (at.count <= 0) return g;
+    if (e.r_f32 && sizeof(T) != 4) {
+        const float *const p = (const float *)e.r + (at.m * e.ldr + at.n) + down * e.ldr;
+#pragma unroll
+        for (int q = 0; q < W / 4; ++q)
+            if (at.count > 4 * q) g.x[q] = *(const v4f *)(p + 4 * q);
+    } else {
+        g.x[0] = *(const v4f *)((const T *)e.r + (at.m * e.ldr + at.n) + down * e.ldr);
+    }
+    return g;
+}
+
+// z = alpha sum + bias (+ beta r)
+template <typename T>
+__device__ __forceinline__ void argument(float (&v)[kWidth<T>], const float (&bias)[kWidth<T>], float alpha) {
+#pragma unroll
+    for (int i = 0; i < kWidth<T>; ++i) v[i] = fmaf(alpha, v[i], bias[i]);
+}
 template <typename T>
 __device__ __forceinline__ void argument(float (&v)[kWidth<T>], const float (&bias)[kWidth<T>], const Epilogue &e,
-                                         float alpha, const Spot &at, int down, float (&r)[kWidth<T>]) {
+                                         float alpha, const Spot &at, const Rest<kWidth<T>> &g, float (&r)[kWidth<T>]) {
     constexpr int W = kWidth<T>;
+    typedef T vec __attribute__((ext_vector_type(W)));
+    if (e.r_f32 && sizeof(T) != 4) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = fmaf(alpha, v[i], bias[i]);
-    if (e.r) {
-        if (e.r_f32) load_f32((const float *)e.r + (at.m * e.ldr + at.n) + down * e.ldr, at.count, r);
-        else load_row((const T *)e.r + (at.m * e.ldr + at.n) + down * e.ldr, at.count, r);
+        for (int i = 0; i < W; ++i) r[i] = i < at.count ? g.x[i / 4][i % 4] : 0.f;
+    } else {
+        const vec x = __builtin_bit_cast(vec, g.x[0]);
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = fmaf(e.beta, r[i], v[i]);
+        for (int i = 0; i < W; ++i) r[i] = i < at.count ? Type<T>::get(x[i]) : 0.f;
     }
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = fmaf(e.beta, r[i], fmaf(alpha, v[i], bias[i]));
 }
-// see mend()
+// a positive value that its type would round to 0: the type's smallest (see mend())
+template <typename T>
+constexpr float kSmallest = std::is_same_v<T, _Float16> ? 0x1p-24f : 0x1p-126f;
 template <typename T>
 __device__ __forceinline__ float above_zero(float y) {
-    constexpr float smallest = std::is_same_v<T, _Float16> ? 0x1p-24f : 0x1p-126f;
-    return y > 0.f && Type<T>::get(Type<T>::put(y)) == 0.f ? smallest : y;
+    return y > 0.f && Type<T>::get(Type<T>::put(y)) == 0.f ? kSmallest<T> : y;
 }
 
 // y = act(z)
@@ -550,10 +587,6 @@ __device__ __forceinline__ void leave(float (&v)[kWidth<T>], const Epilogue &e, 
     if (e.pre) store_row((T *)e.pre + (at.m * e.ldpre + at.n) + down * e.ldpre, at.count, v, e.stream);
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = act_of<ACT>(v[i]);
-    if (ACT == kRelu && e.sure) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = above_zero<T>(v[i]);
-    }
     if (e.y_f32) store_f32((float *)e.y + (at.m * e.ldy + at.n) + down * e.ldy, at.count, v);
     else store_row((T *)e.y + (at.m * e.ldy + at.n) + down * e.ldy, at.count, v, e.stream);
 }
@@ -578,7 +611,9 @@ __device__ __forceinline__ double dot64(const Product &p, int b_cols, int m, int
         load_row(a + k, p.k - k, x);
         if (b_cols) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) y[i] = k + i < p.k ? Type<T>::get(((const T *)p.b)[(k + i) * p.ldb + n]) : 0.f;
+            for (int i = 0; i < W; ++i) y[i] = Type<T>::get(((const T *)p.b)[min(k + i, p.k - 1) * p.ldb + n]);
+#pragma unroll
+            for (int i = 0; i < W; ++i) y[i] = k + i < p.k ? y[i] : 0.f;
         } else {
             load_row((const T *)p.b + n * p.ldb + k, p.k - k, y);
         }
@@ -629,16 +664,26 @@ __device__ __forceinline__ void mend(const Product &p, const Epilogue &e, float 
 struct Unsure {
     Again *list;
     int count = 0;  // the same in all lanes
-    // all lanes call it
+    // Values above zero also leave as such (above_zero). All lanes call it; most,
+    // eight values at a time, with nothing near zero.
     template <typename T>
-    __device__ __forceinline__ void note(const float (&z)[kWidth<T>], const float (&sum)[kWidth<T>],
+    __device__ __forceinline__ void note(float (&z)[kWidth<T>], const float (&sum)[kWidth<T>],
                                          const float (&bias)[kWidth<T>], const float (&r)[kWidth<T>],
                                          const Epilogue &e, float doubt, uint32_t place, int width) {
         constexpr int W = kWidth<T>;
+        float low = INFINITY, added = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            low = fminf(low, fabsf(z[i]));
+            added = fmaxf(added, fmaf(fabsf(e.beta), fabsf(r[i]), fabsf(bias[i])));
+        }
+        if (!__ballot(width > 0 && low < fmaxf(fmaf(added, 0x1p-22f, doubt), kSmallest<T>))) return;
         uint32_t todo = 0;
 #pragma unroll
-        for (int i = 0; i < W; ++i)
+        for (int i = 0; i < W; ++i) {
             if (i < width && unsure(z[i], sum[i], fabsf(bias[i]) + fabsf(e.beta * r[i]), doubt)) todo |= 1u << i;
+            z[i] = above_zero<T>(z[i]);
+        }
         while (const uint64_t who = __ballot(todo != 0)) {
             const int at = count + __popcll(who & ((1ull << (threadIdx.x & 63)) - 1));
             const int first = __ffs((int)todo) - 1;
@@ -652,10 +697,11 @@ struct Unsure {
     }
 };
 
-// f(the activation as a constant): one test a block
-template <typename F>
+// f(the activation as a constant): one test a block; GRADIENT: a product of the
+// backward pass, which has none
+template <bool GRADIENT = false, typename F>
 __device__ __forceinline__ void with_act(int act, F f) {
-    switch (act) {
+    switch (GRADIENT ? kNone : act) {
         case kRelu: return f(std::integral_constant<int, kRelu>());
         case kGelu: return f(std::integral_constant<int, kGelu>());
         case kSilu: return f(std::integral_constant<int, kSilu>());
@@ -678,16 +724,23 @@ __device__ __forceinline__ Spot spot_of(const Product &p, int m0, int n0) {
     s.count = p.n - s.n;
     return s;
 }
-template <typename G, int W, typename F>
-__device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *lds, F f) {
+// What fetch(down) reads for f goes out for four calls together, the first four
+// before the rows pass through LDS: one by one behind the stores of the row before (which
+// the compiler must keep in order) a residual took 6.5 us of 43 at 5003 x 1021 x 2045.
+template <typename G, int W, typename Fetch, typename F>
+__device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *lds, Fetch fetch, F f) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     constexpr int COLS = G::TB * 32, LD = COLS + 4;
     static_assert(32 * LD * 4 * (G::THREADS / 64) <= G::LDS, "the waves' rows");
     float *const slab = (float *)lds + wave * (32 * LD);
     constexpr int LANES = COLS / W, ROWS = 64 / LANES;  // lanes a row, rows at a time
+    constexpr int CALLS = 32 / ROWS, AHEAD = CALLS < 4 ? CALLS : 4;
     const int c = (lane % LANES) * W;
 #pragma unroll
     for (int i = 0; i < G::TA; ++i) {
+        decltype(fetch(0)) got[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) got[u] = fetch(i * 32 + u * ROWS);
 #pragma unroll
         for (int j = 0; j < G::TB; ++j)
 #pragma unroll
@@ -699,21 +752,33 @@ __device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *l
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-#pragma unroll 4
-        for (int u = 0; u < 32 / ROWS; ++u) {
-            const int row = u * ROWS + lane / LANES;
-            float v[W];
+#pragma unroll 1
+        for (int u0 = 0; u0 < CALLS; u0 += AHEAD) {
+            if (u0 > 0) {
 #pragma unroll
-            for (int q = 0; q < W / 4; ++q) {
-                const v4f x = *(const v4f *)(slab + row * LD + c + 4 * q);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[4 * q + r] = x[r];
+                for (int u = 0; u < AHEAD; ++u) got[u] = fetch(i * 32 + (u0 + u) * ROWS);
             }
-            f(i * 32 + u * ROWS, v);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int row = (u0 + u) * ROWS + lane / LANES;
+                float v[W];
+#pragma unroll
+                for (int q = 0; q < W / 4; ++q) {
+                    const v4f x = *(const v4f *)(slab + row * LD + c + 4 * q);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[4 * q + r] = x[r];
+                }
+                f(i * 32 + (u0 + u) * ROWS, v, got[u]);
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
+}
+struct Nothing {};
+template <typename G, int W, typename F>
+__device__ __forceinline__ void by_rows(const v16f (&acc)[G::TA][G::TB], char *lds, F f) {
+    by_rows<G, W>(acc, lds, [](int) { return Nothing(); }, [&](int down, float (&v)[W], Nothing) { f(down, v); });
 }
 
 // The product with the linear epilogue; with more than one split the raw sums
@@ -759,23 +824,36 @@ __global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilo
     constexpr int SLABS = 32 * (G::TB * 32 + 4) * 4 * (C::THREADS / 64);
     static_assert(SLABS + kBudget * (int)sizeof(Again) * (C::THREADS / 64) <= G::LDS, "the waves' rows and lists");
     Unsure again{(Again *)(lds + SLABS) + kBudget * (threadIdx.x >> 6)};
-    with_act(e.act, [&](auto act) {
+    with_act<AC>(e.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
-        by_rows<G, W>(acc, lds, [&](int down, float (&v)[W]) {
-            const bool live = at.count > 0 && at.m + down < p.m;
-            if (ACT != kRelu && !live) return;
-            float sum[W], r[W];
+        // whole: no residual, and all rows and columns of the tile exist, which is
+        // one test a block instead of several a row (716,847 x 300 x 512 fp32: 1,580
+        // us, 1,632 with them). Not for the activations whose arithmetic is the time.
+        const auto rows = [&](auto whole, auto fetch) {
+            by_rows<G, W>(acc, lds, fetch, [&](int down, float (&v)[W], const auto &rest) {
+                const Spot spot{at.m, at.n, whole ? W : at.count};
+                const bool live = whole || (at.count > 0 && at.m + down < p.m);
+                if (ACT != kRelu && !live) return;
+                float sum[W], r[W];
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                sum[i] = v[i];
-                r[i] = 0.f;
-            }
-            if (live) argument<T>(v, bias, e, alpha, at, down, r);
-            if (!AC && ACT == kRelu && sure)
-                again.note<T>(v, sum, bias, r, e, doubt, (uint32_t)(at.m + down - o.m * BM) << 16 | (at.n - o.n * BN),
-                              live ? at.count : 0);
-            if (live) leave<T, ACT>(v, e, at, down);
-        });
+                for (int i = 0; i < W; ++i) {
+                    sum[i] = v[i];
+                    r[i] = 0.f;
+                }
+                if constexpr (std::is_same_v<decltype(rest), const Nothing &>) argument<T>(v, bias, alpha);
+                else argument<T>(v, bias, e, alpha, spot, rest, r);
+                if (!AC && ACT == kRelu && sure)
+                    again.note<T>(v, sum, bias, r, e, doubt,
+                                  (uint32_t)(at.m + down - o.m * BM) << 16 | (at.n - o.n * BN), live ? spot.count : 0);
+                if (live) leave<T, ACT>(v, e, spot, down);
+            });
+        };
+        if constexpr (ACT == kNone || ACT == kRelu) {
+            if (!e.r && (o.m + 1) * BM <= p.m && (o.n + 1) * BN <= p.n)
+                return rows(std::true_type(), [](int) { return Nothing(); });
+        }
+        rows(std::false_type(),
+             [&](int down) { return e.r && at.m + down < p.m ? fetch_rest<T>(e, at, down) : Rest<W>{}; });
     });
     if (!AC && again.count > 0) {
         // behind the rows' own stores
@@ -836,7 +914,8 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
     }
     if (live) {
         load_bias<T>(e.bias, e.bias_f32, n, count, bias);
-        argument<T>(v, bias, e, alpha, spot, 0, r);
+        if (e.r) argument<T>(v, bias, e, alpha, spot, fetch_rest<T>(e, spot, 0), r);
+        else argument<T>(v, bias, alpha);
     }
     const bool sure = e.act == kRelu && e.sure;
     __shared__ Again lists[4][kBudget];
@@ -959,47 +1038,76 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
     __shared__ __attribute__((aligned(1024))) char lds[G::LDS];
     const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     const Place o = place(tm, tn, 1);
+    static_assert(G::THREADS >= BM && G::THREADS >= BN, "a row and a class each");
+    const int tid = threadIdx.x;
+    // a row's class and a class's bias, on their way while the logits are formed
+    int64_t own_class = -1;
+    float class_bias = 0.f;
+    if (tid < BM && o.m * BM + tid < p.m) own_class = c.target(o.m * BM + tid);
+    if (tid < BN && o.n * BN + tid < p.n && c.bias) class_bias = bias_at<T>(c.bias, c.bias_f32, o.n * BN + tid);
     v16f acc[G::TA][G::TB];
     G::product(acc, p, lds, o.m * BM, o.n * BN, 0, (p.k + G::BK - 1) / G::BK);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int wm = wave / WN, wn = wave % WN;
-    float *const top = (float *)lds, *const sum = top + WN * BM;
+    float *const top = (float *)lds, *const sum = top + WN * BM, *const biases = sum + WN * BM;
+    int *const owns = (int *)(biases + BN);  // the row's own class, counted from the tile's first
+    static_assert((2 * WN * BM + BN + BM) * 4 <= G::LDS, "rows and classes");
+    if (tid < BM) {
+        const int64_t t = own_class - (int64_t)o.n * BN;
+        owns[tid] = own_class < p.n && t >= 0 && t < BN ? (int)t : -1;
+    }
+    // what is past the last class takes no part
+    if (tid < BN) biases[tid] = o.n * BN + tid < p.n ? class_bias : -INFINITY;
+    __syncthreads();
     const int n0 = o.n * BN + wn * G::TB * 32 + 4 * (lane >> 5);  // column of a lane's r = 0, j = 0
     const bool whole = o.n * BN + BN <= p.n;
-    float bias[G::TB][16];
-#pragma unroll
-    for (int j = 0; j < G::TB; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int n = n0 + j * 32 + 8 * (r >> 2) + (r & 3);
-            // what is past the last class takes no part
-            bias[j][r] = n >= p.n ? -INFINITY : c.bias ? bias_at<T>(c.bias, c.bias_f32, n) : 0.f;
-        }
+    const float *const bias = biases + (n0 - o.n * BN);
 #pragma unroll
     for (int i = 0; i < G::TA; ++i) {
         const int row = (wm * G::TA + i) * 32 + (lane & 31), m = o.m * BM + row;
-        const int64_t t = m < p.m ? c.target(m) : -1;
-        // the own class, counted from n0, if it is one of this lane's columns
-        const int at = t >= n0 && t < n0 + G::TB * 32 && t < p.n && (((t - n0) >> 2) & 1) == 0 ? (int)(t - n0) : -1;
-        float mx = -INFINITY, own = 0.f;
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < G::TB; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const v4f b = *(const v4f *)(bias + j * 32 + 8 * q);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[i][j][4 * q + r] = b[r] == -INFINITY ? -INFINITY : acc[i][j][4 * q + r] + b[r];
+                }
+        } else if (c.bias) {
+#pragma unroll
+            for (int j = 0; j < G::TB; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const v4f b = *(const v4f *)(bias + j * 32 + 8 * q);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][4 * q + r] += b[r];
+                }
+        }
+        float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < G::TB; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float v = acc[i][j][r];
-                if (c.bias || !whole) v = bias[j][r] == -INFINITY ? -INFINITY : v + bias[j][r];
-                if (at == j * 32 + 8 * (r >> 2) + (r & 3)) own = v;
-                acc[i][j][r] = v;
-                mx = fmaxf(mx, v);
-            }
-        if (at >= 0) c.own_logit[m] = own;
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc[i][j][r]);
+        // the own class, counted from n0, if it is one of this lane's columns: in few tiles
+        const int at = owns[row] - (n0 - o.n * BN);
+        const bool mine = owns[row] >= 0 && at >= 0 && at < G::TB * 32 && ((at >> 2) & 1) == 0;
+        if (__ballot(mine)) {
+            float own = 0.f;
+#pragma unroll
+            for (int j = 0; j < G::TB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) own = at == j * 32 + 8 * (r >> 2) + (r & 3) ? acc[i][j][r] : own;
+            if (mine) c.own_logit[m] = own;
+        }
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         float s = 0.f;
-        const float base = mx == -INFINITY ? 0.f : mx;  // no class left: exp(-inf) = 0 each
+        const ExpBelow<T> exp(mx == -INFINITY ? 0.f : mx);  // no class left: exp(-inf) = 0 each
 #pragma unroll
         for (int j = 0; j < G::TB; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s += exp_of<T>(acc[i][j][r] - base);
+            for (int r = 0; r < 16; ++r) s += exp(acc[i][j][r]);
         s += __shfl_xor(s, 32);
         if (lane < 32) {
             top[wn * BM + row] = mx;
@@ -1030,7 +1138,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
         const float base = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
         for (int w = 0; w < WN; ++w) s += sum[w * BM + row] * expf(top[w * BM + row] - base);
-        const float lse = mx + logf(s);
+        const ExpBelow<T> exp(mx + logf(s));
         const int64_t t = m < p.m ? c.target(m) : -1;
         const bool left_out = m >= p.m || c.left_out(m), bad = !left_out && (t < 0 || t >= p.n);
 #pragma unroll
@@ -1038,7 +1146,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int n = n0 + j * 32 + 8 * (r >> 2) + (r & 3);
-                const float g = c.scale * (exp_of<T>(acc[i][j][r] - lse) - (n == t ? 1.f : 0.f));
+                const float g = c.scale * (exp(acc[i][j][r]) - (n == t ? 1.f : 0.f));
                 acc[i][j][r] = left_out ? 0.f : bad ? NAN : g;
             }
     }
@@ -1060,20 +1168,45 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
     __shared__ __attribute__((aligned(1024))) char lds[G::LDS];
     const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     const Place o = place(tm, tn, 1);
+    static_assert(G::THREADS >= BM, "a row each");
+    const int tid = threadIdx.x;
+    // a row's class, factor and log-sum-exp, on their way while the logits are formed
+    int64_t own_class = -1;
+    float weight = 0.f, lse = 0.f;
+    if (tid < BM && o.m * BM + tid < p.m) {
+        own_class = c.target(o.m * BM + tid);
+        weight = c.weight[o.m * BM + tid];
+        lse = c.lse[o.m * BM + tid];
+    }
     v16f acc[G::TA][G::TB];
     G::product(acc, p, lds, o.m * BM, o.n * BN, 0, (p.k + G::BK - 1) / G::BK);
+    struct Row {
+        float weight, base;
+        int own;  // counted from the tile's first class
+    };
+    constexpr int SLABS = 32 * (G::TB * 32 + 4) * 4 * (C::THREADS / 64);
+    static_assert(SLABS + BM * (int)sizeof(Row) <= G::LDS, "the waves' rows and theirs");
+    Row *const rows = (Row *)(lds + SLABS);
+    if (tid < BM) {
+        const int64_t t = own_class - c.first - (int64_t)o.n * BN;
+        rows[tid] = Row{weight * c.scale, lse, own_class >= 0 && t >= 0 && t < BN ? (int)t : -1};
+    }
+    __syncthreads();
     const Spot at = spot_of<G, W>(p, o.m * BM, o.n * BN);
     float bias[W];
     load_bias<T>(c.bias, c.bias_f32, at.n, at.count, bias);
     by_rows<G, W>(acc, lds, [&](int down, float (&v)[W]) {
         const int m = at.m + down;
         if (m >= p.m || at.count <= 0) return;
-        const int64_t t = c.target(m) - c.first - at.n;  // the own class among the lane's columns
-        const float w = c.weight[m] * c.scale, lse = c.lse[m];
+        const Row row = rows[m - o.m * BM];
+        const ExpBelow<T> exp(row.base);
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float g = w * (exp_of<T>(v[i] + bias[i] - lse) - (i == t ? 1.f : 0.f));
-            v[i] = w == 0.f ? 0.f : g;
+        for (int i = 0; i < W; ++i) v[i] = row.weight == 0.f ? 0.f : row.weight * exp(v[i] + bias[i]);
+        const int own = row.own - (at.n - o.n * BN);  // the own class among the lane's columns
+        if (row.own >= 0 && own >= 0 && own < W) {
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (i == own) v[i] -= row.weight;
         }
         store_row((T *)c.grad + (at.m * c.ldgrad + at.n) + down * c.ldgrad, at.count, v);
     });
