@@ -541,8 +541,8 @@ typedef struct {
     int32_t for_gradients; /* Y will be given to rsc_linear_backward */
 } rsc_linear_t;
 
-/* rsc_linear: bias, R and pre may be NULL; pre (n x m) receives Z, which the
- * backward pass of GELU and SiLU needs. Y may be R (in place) but must not
+/* rsc_linear: bias, R and pre may be NULL; pre (n x m, fp32) receives Z, which
+ * the backward pass of GELU and SiLU needs. Y may be R (in place) but must not
  * overlap X or W. fp32 products are formed from three bf16 parts a value
  * (24 bits in all, six partial products): finite operands of magnitude below
  * 3.3e38 give fp32 accuracy; an infinite operand gives NaN.
@@ -550,11 +550,12 @@ typedef struct {
 size_t rsc_linear_workspace_bytes(const rsc_linear_t *p);
 rsc_status_t rsc_linear(const rsc_linear_t *p, const void *X, int64_t ldx, const void *W, int64_t ldw,
                         const void *bias, int32_t bias_dtype, const void *R, int64_t ldr, void *Y, int64_t ldy,
-                        void *pre, int64_t ldpre, void *ws, size_t ws_bytes, hipStream_t stream);
+                        float *pre, int64_t ldpre, void *ws, size_t ws_bytes, hipStream_t stream);
 /* Gradients for dY: dZ = dY act'(Z), dX = alpha dZ W^T, dW = alpha X^T dZ
  * (stored as W is), dbias = sum over rows of dZ, dR = beta dZ; each output
- * may be NULL (X may be NULL without dW, W without dX). dZ is held in the operands' type. saved: Y for ReLU (its slope is 1
- * where Y > 0), pre for GELU and SiLU, unused (NULL) without an activation.
+ * may be NULL (X may be NULL without dW, W without dX). dZ is held in the
+ * operands' type. saved: Y for ReLU (its slope is 1 where Y > 0), pre for GELU
+ * and SiLU, unused (NULL) without an activation.
  * n = 0 gives zero dW and dbias. The workspace holds dZ (with an activation),
  * partial sums of dbias and of split products; its size covers the outputs
  * named by the flags. */

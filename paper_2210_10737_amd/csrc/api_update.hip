@@ -140,14 +140,14 @@ size_t rsc_linear_workspace_bytes(const rsc_linear_t *p) {
 
 rsc_status_t rsc_linear(const rsc_linear_t *p, const void *X, int64_t ldx, const void *W, int64_t ldw,
                         const void *bias, int32_t bias_dtype, const void *R, int64_t ldr, void *Y, int64_t ldy,
-                        void *pre, int64_t ldpre, void *ws, size_t ws_bytes, hipStream_t stream) {
+                        float *pre, int64_t ldpre, void *ws, size_t ws_bytes, hipStream_t stream) {
     RSC_TRY(check_linear(p));
     RSC_TRY(check_matrix(X, p->n, p->k, ldx, p->dtype, "X"));
     RSC_TRY(check_matrix(W, 1, p->w_out_major ? p->k : p->m, ldw, p->dtype, "W"));
     RSC_TRY(check_vector(bias, bias_dtype, p->dtype, "bias"));
     if (R) RSC_TRY(check_matrix(R, p->n, p->m, ldr, p->dtype, "R"));
     RSC_TRY(check_matrix(Y, p->n, p->m, ldy, p->dtype, "Y"));
-    if (pre) RSC_TRY(check_matrix(pre, p->n, p->m, ldpre, p->dtype, "pre"));
+    if (pre) RSC_TRY(check_matrix(pre, p->n, p->m, ldpre, RSC_F32, "pre"));
     if (p->n > 0 && (Y == X || Y == W || (pre && (pre == Y || pre == X || pre == W))))
         return fail(RSC_ERR_INVALID_ARGUMENT, "an output of the layer is one of its operands");
     if (p->n == 0) return RSC_OK;
@@ -172,7 +172,7 @@ rsc_status_t rsc_linear_backward(const rsc_linear_t *p, const void *dY, int64_t 
     RSC_TRY(check_linear(p));
     const int64_t w_rows = p->w_out_major ? p->m : p->k, w_cols = p->w_out_major ? p->k : p->m;
     RSC_TRY(check_matrix(dY, p->n, p->m, lddy, p->dtype, "dY"));
-    if (p->act != RSC_ACT_NONE) RSC_TRY(check_matrix(saved, p->n, p->m, ldsaved, p->dtype, "saved"));
+    if (p->act != RSC_ACT_NONE) RSC_TRY(check_matrix(saved, p->n, p->m, ldsaved, p->act == RSC_ACT_RELU ? p->dtype : RSC_F32, "saved"));
     if (dW) {
         RSC_TRY(check_matrix(X, p->n, p->k, ldx, p->dtype, "X"));
         RSC_TRY(check_matrix(dW, w_rows, w_cols, lddw, p->dtype, "dW"));

@@ -500,11 +500,11 @@ __device__ __forceinline__ void load_f32(const float *p, int count, float (&v)[W
     }
 }
 template <int W>
-__device__ __forceinline__ void store_f32(float *p, int count, const float (&v)[W]) {
+__device__ __forceinline__ void store_f32(float *p, int count, const float (&v)[W], bool stream = false) {
 #pragma unroll
     for (int q = 0; q < W / 4; ++q) {
         const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-        store_row(p + 4 * q, count - 4 * q, x);
+        store_row(p + 4 * q, count - 4 * q, x, stream);
     }
 }
 
@@ -584,7 +584,7 @@ __device__ __forceinline__ float above_zero(float y) {
 template <typename T, int ACT>
 __device__ __forceinline__ void leave(float (&v)[kWidth<T>], const Epilogue &e, const Spot &at, int down) {
     constexpr int W = kWidth<T>;
-    if (e.pre) store_row((T *)e.pre + (at.m * e.ldpre + at.n) + down * e.ldpre, at.count, v, e.stream);
+    if (e.pre) store_f32(e.pre + (at.m * e.ldpre + at.n) + down * e.ldpre, at.count, v, e.stream);
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] = act_of<ACT>(v[i]);
     if (e.y_f32) store_f32((float *)e.y + (at.m * e.ldy + at.n) + down * e.ldy, at.count, v);
@@ -653,7 +653,7 @@ __device__ __forceinline__ void mend(const Product &p, const Epilogue &e, float 
     if (e.r) s += (double)e.beta * (double)r;
     if ((threadIdx.x & 63) != 0) return;
     const float z = (float)s, y = above_zero<T>(fmaxf(z, 0.f));
-    if (e.pre) ((T *)e.pre)[m * e.ldpre + n] = Type<T>::put(z);
+    if (e.pre) e.pre[m * e.ldpre + n] = z;
     if (e.y_f32) ((float *)e.y)[m * e.ldy + n] = y;
     else ((T *)e.y)[m * e.ldy + n] = Type<T>::put(y);
 }
@@ -1021,7 +1021,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(Product p, Epilogue e) {
         exact += (double)e.beta * (double)r;
     }
     if (sure) v = (float)exact;
-    if (e.pre) ((T *)e.pre)[m * e.ldpre + n] = Type<T>::put(v);
+    if (e.pre) e.pre[m * e.ldpre + n] = v;
     with_act(e.act, [&](auto act) { v = act_of<decltype(act)::value>(v); });
     if (sure) v = above_zero<T>(v);
     if (e.y_f32) ((float *)e.y)[m * e.ldy + n] = v;

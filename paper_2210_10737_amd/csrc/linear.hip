@@ -26,7 +26,8 @@ struct Val<_Float16> {
 };
 
 // act'(z) from what the forward pass kept: the output for a ReLU (positive
-// where the argument was), the argument itself for the others
+// where the argument was), the argument itself, in fp32, for the others: rounded
+// to 16 bits it added a tenth to a gradient's error.
 __device__ __forceinline__ float slope_of(float s, int act) {
     switch (act) {
         case kRelu: return s > 0.f ? 1.f : (s != s ? s : 0.f);
@@ -44,7 +45,10 @@ __device__ __forceinline__ float slope_of(float s, int act) {
 }
 
 // One pass over dY: dz = dY act'(saved), dr = beta dz, and the column sums of
-// dz over this block's rows, in fp64 (the additions hide behind the loads).
+// dz over this block's rows, in fp64 (the additions hide behind the loads). dz is
+// rounded to the operands' type, for the matrix instructions: for 16 bits dX and dW are
+// then off by sqrt(2) times their own rounding, behind GELU and SiLU (a ReLU's
+// dz is dY or 0). A second product for the rest would double the pass.
 // A block takes `strip` columns, as groups of W values a thread, and the rows
 // of its chunk; any of dz, dr and part may be missing.
 struct Pass {
@@ -103,11 +107,21 @@ __global__ __launch_bounds__(256) void pass_kernel(Pass p) {
         typedef T vec __attribute__((ext_vector_type(W)));
         for (int64_t r = r0 + lane; r < r1; r += 4 * lanes) {
             vec y[4], z[4];
+            float4 zf[4][W / 4];
+            // kept in T (a ReLU's output) or in fp32
+            const bool same = p.act == kRelu || (p.act != kNone && sizeof(T) == 4);
+            const bool wide = p.act != kNone && !same;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int64_t row = min(r + u * lanes, r1 - 1);
                 y[u] = *(const vec *)((const T *)p.dy + row * p.lddy + c);
-                if (p.act != kNone) z[u] = *(const vec *)((const T *)p.saved + row * p.ldsaved + c);
+                if (same) z[u] = *(const vec *)((const T *)p.saved + row * p.ldsaved + c);
+                if (wide) {
+                    // (the row's 16-byte units; past the last one it is read again)
+                    const float4 *const from = (const float4 *)((const float *)p.saved + row * p.ldsaved + c);
+#pragma unroll
+                    for (int q = 0; q < W / 4; ++q) zf[u][q] = from[count > 4 * q ? q : 0];
+                }
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -116,7 +130,9 @@ __global__ __launch_bounds__(256) void pass_kernel(Pass p) {
 #pragma unroll
                 for (int i = 0; i < W; ++i) {
                     v[i] = i < count ? (float)y[u][i] : 0.f;
-                    s[i] = p.act != kNone && i < count ? (float)z[u][i] : 0.f;
+                    s[i] = 0.f;
+                    if (same) s[i] = i < count ? (float)z[u][i] : 0.f;
+                    if (wide) s[i] = i < count ? (&zf[u][i / 4].x)[i % 4] : 0.f;
                 }
                 take(r + u * lanes, v, s);
             }
@@ -308,7 +324,7 @@ size_t linear_ws_bytes(const Linear &l) {
 }
 
 hipError_t linear_launch(const Linear &l, const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias,
-                         int32_t bias_f32, const void *r, int64_t ldr, void *y, int64_t ldy, void *pre, int64_t ldpre,
+                         int32_t bias_f32, const void *r, int64_t ldr, void *y, int64_t ldy, float *pre, int64_t ldpre,
                          void *ws, hipStream_t stream) {
     Product p;
     p.a = x;

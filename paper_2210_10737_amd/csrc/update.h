@@ -36,7 +36,7 @@ struct Epilogue {
     int32_t y_f32 = 0;
     void *y = nullptr;
     int64_t ldy = 0;
-    void *pre = nullptr;
+    float *pre = nullptr;
     int64_t ldpre = 0;
     // results go past the caches (set by the launch for large ones)
     bool stream = false;
@@ -117,7 +117,7 @@ struct Linear {
 size_t linear_ws_bytes(const Linear &l);
 size_t linear_backward_ws_bytes(const Linear &l, bool dx, bool dw, bool db);
 hipError_t linear_launch(const Linear &l, const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias,
-                         int32_t bias_f32, const void *r, int64_t ldr, void *y, int64_t ldy, void *pre, int64_t ldpre,
+                         int32_t bias_f32, const void *r, int64_t ldr, void *y, int64_t ldy, float *pre, int64_t ldpre,
                          void *ws, hipStream_t stream);
 struct LinearGrads {
     void *dx = nullptr, *dw = nullptr, *db = nullptr, *dr = nullptr;
