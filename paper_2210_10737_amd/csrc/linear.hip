@@ -48,7 +48,8 @@ __device__ __forceinline__ float slope_of(float s, int act) {
 // dz over this block's rows, in fp64 (the additions hide behind the loads). dz is
 // rounded to the operands' type, for the matrix instructions: for 16 bits dX and dW are
 // then off by sqrt(2) times their own rounding, behind GELU and SiLU (a ReLU's
-// dz is dY or 0). A second product for the rest would double the pass.
+// dz is dY or 0). A second product for the rest would double the pass. Bound by
+// memory: 232,965 x 256 fp32 with GELU 164 us, 4.4 TB/s.
 // A block takes `strip` columns, as groups of W values a thread, and the rows
 // of its chunk; any of dz, dr and part may be missing.
 struct Pass {
@@ -246,7 +247,9 @@ hipError_t zero_launch(int32_t dtype, void *p, int64_t ld, int64_t rows, int64_t
 // A model of the time in nanoseconds: blocks run in rounds of as many as the
 // 256 CUs hold, a block's tiles of k at the rate its shape reaches and a fixed
 // part for its first loads and its results; splits add a launch and the
-// writing and reading of their partial sums.
+// writing and reading of their partial sums. The rates are those of products
+// forced to each shape, 1 to 700,000 rows. For 5003 x 1021 x 2045 fp16 it picks 256 x 256
+// (38 us; 44 with 128 x 128, 41 with 128 x 64), for dX of the same layer 128 x 64 (36 us).
 namespace {
 Cut cut_of(int32_t dtype, int64_t m, int64_t n, int64_t k, bool may_split) {
     // flops per ns of a CU with all its blocks, blocks a CU, ns of a block
