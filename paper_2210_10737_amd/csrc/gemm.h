@@ -812,13 +812,18 @@ __global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilo
     const bool sure = !AC && e.act == kRelu && e.sure;  // (the forward pass)
     float doubt = -1.f;  // (nothing is unsure)
     if (sure) {
+        // Columns past the last take no part: with B stored by columns they are sums
+        // of what lies beside a row in memory.
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        const int left = p.n - (o.n * BN + (wave % C::WN) * G::TB * 32 + 4 * (lane >> 5));
         float largest = 0.f;
 #pragma unroll
         for (int i = 0; i < G::TA; ++i)
 #pragma unroll
             for (int j = 0; j < G::TB; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(acc[i][j][r]));
+                for (int r = 0; r < 16; ++r)
+                    largest = j * 32 + 8 * (r >> 2) + (r & 3) < left ? fmaxf(largest, fabsf(acc[i][j][r])) : largest;
         doubt = doubt_of(fabsf(alpha) * wave_max(largest), p.k);
     }
     constexpr int SLABS = 32 * (G::TB * 32 + 4) * 4 * (C::THREADS / 64);

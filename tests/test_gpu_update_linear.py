@@ -357,3 +357,22 @@ def test_relu_masks_of_cancelled_sums():
         want = rsc.linear(x.clone().requires_grad_(), w, b, residual=r, act="relu").detach()
         y, _, _, _ = update._linear_forward(x, w, b, r, 1, 1.0, 1.0, r, True)
         assert y is r and torch.equal(y, want), size
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(700, 520, 301), (300, 64, 41), (9000, 130, 300), (3000, 64, 5)])
+def test_relu_with_gradients_does_not_depend_on_what_lies_beside_the_weights(size, dtype):
+    """Large values beside the weights' rows, as an uninitialised or a wider
+    buffer may hold them: results are those beside zeros, bit for bit."""
+    n, k, m = size
+    x, w, b, r, _ = inputs(n, k, m, dtype, False, 12)
+    wide = torch.zeros((k, (m + 31) // 16 * 16), dtype=dtype, device="cuda")
+    wide[:, :m] = w
+    assert update._ld(wide[:, :m]) is not None       # used as it lies
+    got = []
+    for beside in (0.0, 1e30 if dtype != torch.float16 else 6e4, float("inf"), float("nan")):
+        wide[:, m:] = beside
+        for residual in (None, r):
+            got.append(rsc.linear(x.clone().requires_grad_(), wide[:, :m], b, residual=residual, act="relu").detach())
+    for i, y in enumerate(got[2:]):
+        assert torch.equal(y, got[i % 2]), i
