@@ -530,8 +530,8 @@ typedef enum { RSC_ACT_NONE = 0, RSC_ACT_RELU = 1, RSC_ACT_GELU = 2, RSC_ACT_SIL
  *   act: none, max(z, 0), z Phi(z) (the exact GELU), z / (1 + exp(-z)).
  *   for_gradients: with ReLU, the sign of results next to zero, on which
  *   gradients hang, is decided by sums in 64 bits (at most 32 in each group of
- *   some thousand results), and a positive one does not round to 0; without
- *   effect otherwise. */
+ *   some thousand results; next to zero beside the largest result of the same
+ *   row), and a positive one does not round to 0; without effect otherwise. */
 typedef struct {
     int32_t dtype; /* rsc_dtype_t of X, W, R, Y */
     int32_t act;   /* rsc_act_t */

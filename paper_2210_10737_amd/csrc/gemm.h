@@ -625,9 +625,13 @@ __device__ __forceinline__ double dot64(const Product &p, int b_cols, int m, int
     return sum;
 }
 
-// how far a sum of k terms may be off beside the largest sum around it: a
+// How far a sum of k terms may be off, from the largest sum of its row near by: a
 // random walk of roundings takes it 2^-24 sqrt(k / 16) of that, this is more
-// than ten times as far
+// than ten times as far. By rows, since rows of A may differ by any factor: under
+// the largest sum of all, one row takes the whole list for its neighbours. From
+// fewer than kScaleOf columns a row's scale does not show (all of them may be next
+// to zero), and the wave's largest sum stands for it.
+constexpr int kScaleOf = 8;
 __device__ __forceinline__ float doubt_of(float largest, int k) { return largest * 0x1p-24f * (8.f + sqrtf((float)k)); }
 
 // Is an argument next to zero? `others`: the magnitudes added to the sum. A sum
@@ -810,25 +814,34 @@ __global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilo
     float bias[W];
     load_bias<T>(e.bias, e.bias_f32, at.n, at.count, bias);
     const bool sure = !AC && e.act == kRelu && e.sure;  // (the forward pass)
-    float doubt = -1.f;  // (nothing is unsure)
+    // in LDS behind the waves' rows: each wave's list, and its rows' bounds
+    constexpr int SLABS = 32 * (G::TB * 32 + 4) * 4 * (C::THREADS / 64), LISTS = kBudget * (int)sizeof(Again) * (C::THREADS / 64);
+    static_assert(SLABS + LISTS + G::TA * 32 * 4 * (C::THREADS / 64) <= G::LDS, "the waves' rows, lists and bounds");
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    Unsure again{(Again *)(lds + SLABS) + kBudget * wave};
+    float *const doubts = (float *)(lds + SLABS + LISTS) + G::TA * 32 * wave;
     if (sure) {
         // Columns past the last take no part: with B stored by columns they are sums
         // of what lies beside a row in memory.
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
         const int left = p.n - (o.n * BN + (wave % C::WN) * G::TB * 32 + 4 * (lane >> 5));
-        float largest = 0.f;
+        float largest[G::TA], all = 0.f;
 #pragma unroll
-        for (int i = 0; i < G::TA; ++i)
+        for (int i = 0; i < G::TA; ++i) {
+            largest[i] = 0.f;
 #pragma unroll
             for (int j = 0; j < G::TB; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    largest = j * 32 + 8 * (r >> 2) + (r & 3) < left ? fmaxf(largest, fabsf(acc[i][j][r])) : largest;
-        doubt = doubt_of(fabsf(alpha) * wave_max(largest), p.k);
+                    largest[i] = j * 32 + 8 * (r >> 2) + (r & 3) < left ? fmaxf(largest[i], fabsf(acc[i][j][r])) : largest[i];
+            largest[i] = fmaxf(largest[i], __shfl_xor(largest[i], 32));
+            all = fmaxf(all, largest[i]);
+        }
+        const bool few = p.n - (o.n * BN + (wave % C::WN) * G::TB * 32) < kScaleOf;
+        if (few) all = wave_max(all);
+#pragma unroll
+        for (int i = 0; i < G::TA; ++i)
+            doubts[i * 32 + (lane & 31)] = doubt_of(fabsf(alpha) * (few ? all : largest[i]), p.k);
     }
-    constexpr int SLABS = 32 * (G::TB * 32 + 4) * 4 * (C::THREADS / 64);
-    static_assert(SLABS + kBudget * (int)sizeof(Again) * (C::THREADS / 64) <= G::LDS, "the waves' rows and lists");
-    Unsure again{(Again *)(lds + SLABS) + kBudget * (threadIdx.x >> 6)};
     with_act<AC>(e.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
         // whole: no residual, and all rows and columns of the tile exist, which is
@@ -848,7 +861,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilo
                 if constexpr (std::is_same_v<decltype(rest), const Nothing &>) argument<T>(v, bias, alpha);
                 else argument<T>(v, bias, e, alpha, spot, rest, r);
                 if (!AC && ACT == kRelu && sure)
-                    again.note<T>(v, sum, bias, r, e, doubt,
+                    again.note<T>(v, sum, bias, r, e, doubts[at.m + down - o.m * BM - (wave / C::WN) * G::TA * 32],
                                   (uint32_t)(at.m + down - o.m * BM) << 16 | (at.n - o.n * BN), live ? spot.count : 0);
                 if (live) leave<T, ACT>(v, e, spot, down);
             });
@@ -929,7 +942,25 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
         float largest = 0.f;
 #pragma unroll
         for (int i = 0; i < W; ++i) largest = fmaxf(largest, fabsf(sum[i]));
-        const float doubt = doubt_of(fabsf(alpha) * wave_max(largest), p.k);
+        // over the wave's chunks of the same row, which are next to each other
+        // (places past the last have sums of 0)
+        const float all = wave_max(largest);
+        const int64_t first = ((int64_t)blockIdx.x * 256 + (threadIdx.x & ~63)) / L;
+        const int from_chunk = (int)max((int64_t)0, first - m * chunks), to_chunk = (int)min(chunks, first + 64 / L - m * chunks);
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const float below = __shfl_up(largest, d);
+            const int row = __shfl_up(m, d);
+            if ((int)(threadIdx.x & 63) >= d && row == m) largest = fmaxf(largest, below);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const float above = __shfl_down(largest, d);
+            const int row = __shfl_down(m, d);
+            if ((int)(threadIdx.x & 63) + d < 64 && row == m) largest = fmaxf(largest, above);
+        }
+        const bool few = min(to_chunk * W, p.n) - from_chunk * W < kScaleOf;
+        const float doubt = doubt_of(fabsf(alpha) * (few ? all : largest), p.k);
         // places: the value's number among the wave's
         again.note<T>(v, sum, bias, r, e, doubt, (threadIdx.x & 63) * W, live ? count : 0);
     }

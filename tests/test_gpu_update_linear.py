@@ -376,3 +376,24 @@ def test_relu_with_gradients_does_not_depend_on_what_lies_beside_the_weights(siz
             got.append(rsc.linear(x.clone().requires_grad_(), wide[:, :m], b, residual=residual, act="relu").detach())
     for i, y in enumerate(got[2:]):
         assert torch.equal(y, got[i % 2]), i
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(4992, 300, 320), (704, 1021, 320), (64, 9000, 320), (320, 300, 64)])
+def test_relu_masks_beside_rows_of_another_scale(size, dtype):
+    """One row in 32 is 2^14 times as large as the others, whose sums are 0.06 or
+    so. Every fourth column's bias takes the sum of one ordinary row away but its
+    rounding: that row's result is decided in 64 bits, as among rows of one scale."""
+    n, k, m = size
+    g = torch.Generator(device="cuda").manual_seed(21)
+    x, w = rand((n, k), dtype, g, 2.0 ** -4), rand((k, m), dtype, g, 1 / math.sqrt(k))
+    x[::32] *= 2.0 ** 14
+    b = rand((m,), torch.float32, g, 2.0 ** -4)
+    exact = x.double() @ w.double()
+    column = torch.arange(0, m, 4, device="cuda")
+    row = (column * 32 + 16 + column % 16) % (n // 32 * 32)
+    b[column] = -exact[row, column].float()
+    y = rsc.linear(x.clone().requires_grad_(), w, b, act="relu").detach()
+    z = exact + b.double()
+    assert bool((z[row, column].abs() <= 2.0 ** -24 * exact[row, column].abs()).all())
+    assert torch.equal(y > 0, z > 0)
