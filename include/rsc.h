@@ -573,7 +573,10 @@ rsc_status_t rsc_linear_backward(const rsc_linear_t *p, const void *dY, int64_t 
  *   targets: n values, int64 or int32 (targets_i32). Rows whose target is
  *   ignore_index are left out: loss 0, gradients 0 (their X rows must still be
  *   finite: they enter dW times 0). Any other target outside 0 .. v-1 gives
- *   NaN. Logits of 16-bit operands must stay below 2.3e38 in magnitude.
+ *   NaN. A bias of -inf or of the lowest finite value takes a class out.
+ *   Probabilities in the gradients are exp(logit - lse) with both in fp32,
+ *   so off by up to 2^-24 of the two magnitudes: they mean nothing in a row
+ *   whose largest logit is itself such a lowest value.
  *   reduction: 0 = loss per row (n values), 1 = sum, 2 = mean over the rows
  *   not left out (0 if there is none). */
 typedef struct {

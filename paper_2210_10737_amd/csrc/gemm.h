@@ -440,18 +440,13 @@ __device__ __forceinline__ float act_of(float z) {
     return z;
 }
 
-// exp(v - base), for many v of one base. For fp32 results to the rounding of
-// fp32; for 16-bit ones by the hardware's power of two (2 ulp), with
-// base log2(e) rounded once: all of a base's results are off by the same factor
-// of at most 1 + |base| 2^-24.
+// exp(v - base). For fp32 results to the rounding of fp32; for 16-bit ones by the
+// hardware's power of two (2 ulp). The difference comes first: log2(e) times a
+// logit of fp32's lowest values, as masks have them, is past its range.
 template <typename T>
-struct ExpBelow {
-    float base;
-    __device__ __forceinline__ explicit ExpBelow(float b) : base(sizeof(T) == 4 ? b : b * 1.44269504089f) {}
-    __device__ __forceinline__ float operator()(float v) const {
-        return sizeof(T) == 4 ? expf(v - base) : __builtin_amdgcn_exp2f(fmaf(v, 1.44269504089f, -base));
-    }
-};
+__device__ __forceinline__ float exp_below(float v, float base) {
+    return sizeof(T) == 4 ? expf(v - base) : __builtin_amdgcn_exp2f((v - base) * 1.44269504089f);
+}
 
 template <typename T>
 __device__ __forceinline__ float bias_at(const void *bias, int f32, int64_t n) {
@@ -1142,11 +1137,11 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
         }
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         float s = 0.f;
-        const ExpBelow<T> exp(mx == -INFINITY ? 0.f : mx);  // no class left: exp(-inf) = 0 each
+        const float base = mx == -INFINITY ? 0.f : mx;  // no class left: exp(-inf) = 0 each
 #pragma unroll
         for (int j = 0; j < G::TB; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s += exp(acc[i][j][r]);
+            for (int r = 0; r < 16; ++r) s += exp_below<T>(acc[i][j][r], base);
         s += __shfl_xor(s, 32);
         if (lane < 32) {
             top[wn * BM + row] = mx;
@@ -1177,7 +1172,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
         const float base = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
         for (int w = 0; w < WN; ++w) s += sum[w * BM + row] * expf(top[w * BM + row] - base);
-        const ExpBelow<T> exp(mx + logf(s));
+        const float lse = mx + logf(s);
         const int64_t t = m < p.m ? c.target(m) : -1;
         const bool left_out = m >= p.m || c.left_out(m), bad = !left_out && (t < 0 || t >= p.n);
 #pragma unroll
@@ -1185,7 +1180,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int n = n0 + j * 32 + 8 * (r >> 2) + (r & 3);
-                const float g = c.scale * (exp(acc[i][j][r]) - (n == t ? 1.f : 0.f));
+                const float g = c.scale * (exp_below<T>(acc[i][j][r], lse) - (n == t ? 1.f : 0.f));
                 acc[i][j][r] = left_out ? 0.f : bad ? NAN : g;
             }
     }
@@ -1240,9 +1235,8 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
         const int m = at.m + down;
         if (m >= p.m || at.count <= 0) return;
         const Row row = rows[m - o.m * BM];
-        const ExpBelow<T> exp(row.base);
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = row.weight == 0.f ? 0.f : row.weight * exp(v[i] + bias[i]);
+        for (int i = 0; i < W; ++i) v[i] = row.weight == 0.f ? 0.f : row.weight * exp_below<T>(v[i] + bias[i], row.base);
         const int own = row.own - (at.n - o.n * BN);  // the own class among the lane's columns
         if (row.own >= 0 && own >= 0 && own < W) {
 #pragma unroll

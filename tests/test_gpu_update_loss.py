@@ -259,3 +259,37 @@ def test_refusals():
         args = {**dict(x=x, weight=w, targets=t, bias=b), **bad}
         with pytest.raises(ValueError):
             rsc.linear_cross_entropy(**args)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lowest", [torch.float32, None])      # of an fp32 bias, or of the operands' type
+@pytest.mark.parametrize("v,masked", [(1500, (300, 1100)), (1500, (0, 1400)), (50, (2, 50)), (50, (0, 40)), (700, (256, 700))])
+def test_long_ranges_of_classes_at_the_lowest_value(v, masked, lowest, dtype):
+    """A bias of the type's lowest value takes a range of classes out that is
+    wider than a tile: loss and gradients are those without these classes."""
+    n, k = 70, 48
+    x, w, b, t = inputs(n, k, v, dtype, True, 0.8, 13)
+    b = b.float() if lowest else b
+    b[masked[0]:masked[1]] = torch.finfo(b.dtype).min
+    rest = torch.cat([torch.arange(masked[0]), torch.arange(masked[1], v)]).cuda()
+    t = torch.where(t >= 0, rest[t.clamp_min(0) % rest.numel()], t)
+    among = torch.where(t >= 0, torch.searchsorted(rest, t.clamp_min(0)), t)
+    up = torch.full((), 1.5, device="cuda")
+    for a in (x, w, b):
+        a.requires_grad_()
+    loss = rsc.linear_cross_entropy(x, w, t, b)
+    rows, rows_bound, grad, grad_off, grad_mag, count = reference(x, w[:, rest], b[rest], among, -100, "mean", up)
+    keep = (t >= 0).double()
+    close(loss.detach(), rows.sum() / count, (rows_bound * keep).sum() / count + 2.0 ** -23 * rows.sum() / count + 1e-7, v)
+    got = torch.autograd.grad(loss, [x, w, b], up)
+    tiny = 1.5 * 2.0 ** -34 if dtype == torch.float16 else 0.0
+    grad_off = grad_off + half(dtype) * grad_mag + tiny * (grad_mag > 0) + 2.0 ** -22 * grad_mag
+    small = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps
+    x6, w6 = x.detach().double(), w.detach()[:, rest].double()
+    want, off = grad @ w6.t(), grad_off @ w6.abs().t() + sums(v) * ((grad_mag + grad_off) @ w6.abs().t())
+    close(got[0], want, off + half(dtype) * (want.abs() + off) + small, "dx")
+    want, off = x6.t() @ grad, x6.abs().t() @ grad_off + sums(n) * (x6.abs().t() @ (grad_mag + grad_off))
+    close(got[1][:, rest], want, off + half(dtype) * (want.abs() + off) + small, "dw")
+    want, off = grad.sum(0), grad_off.sum(0)
+    close(got[2][rest], want, off + half(b.dtype) * (want.abs() + off) + small, "db")
+    assert not got[1][:, masked[0]:masked[1]].any() and not got[2][masked[0]:masked[1]].any()
