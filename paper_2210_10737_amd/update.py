@@ -18,6 +18,7 @@ from array import array
 
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from . import AdamwStruct, LinearStruct, XentStruct, _check, _device_index, _dp, _stream, _workspace, lib
 
@@ -146,6 +147,8 @@ def _linear_forward(x, weight, bias, residual, act: int, alpha: float, beta: flo
                           None if ws is None else ws.data_ptr(), need, _stream())
     if status:
         _check(status)
+    if out is not None:
+        increment_version(out)
     return y, pre, xa, wa
 
 
@@ -201,7 +204,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
     weight's storage order. With gradients a ReLU's sign next to zero is decided
     in 64 bits (at most 32 times in some thousand results), and GELU and SiLU
     keep their argument, n x m float32. out (no gradients): [n, m] with aligned rows, may
-    be the residual."""
+    be the residual; the write counts as one in place to autograd."""
     if act not in _ACTS:
         raise ValueError(f"act {act!r}: none, relu, gelu or silu expected")
     n, _, m = _check_product(x, weight, bias)
@@ -215,6 +218,8 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
         return _Linear.apply(x, weight, bias, residual, _ACTS[act], float(alpha), float(beta))
     if out is not None:
         _check_operand(out, "out", (n, m), x.dtype)
+        if out.requires_grad and torch.is_grad_enabled():
+            raise ValueError("out requires gradients: a write to it is for no_grad")
         if _ld(out) is None:
             raise ValueError("out: rows of whole 16-byte units with unit column stride expected")
     return _linear_forward(x, weight, bias, residual, _ACTS[act], float(alpha), float(beta), out, False)[0]
@@ -359,7 +364,9 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: torch.Tensor, *, lr: 
     float16). Moments: float32, or with both lists of scales 8-bit codes (int8,
     uint8; a float32 scale for each 256 elements). masters: float32 values that
     the step is applied to, params then receive their rounding. step: int64[1]
-    on the device, advanced by the call. No tensor may appear twice."""
+    on the device, advanced by the call. No tensor may appear twice. To autograd
+    the step is a write in place to params and masters: a backward pass of a graph
+    that saved one of them before raises."""
     count = len(params)
     if (exp_avg_scales is None) != (exp_avg_sq_scales is None):
         raise ValueError("8-bit moments need both exp_avg_scales and exp_avg_sq_scales")
@@ -382,6 +389,9 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, step: torch.Tensor, *, lr: 
     need = lib().rsc_adamw_workspace_bytes()
     ws = _workspace(need, step.device)
     _check(lib().rsc_adamw_step(ctypes.byref(opts), array, count, _dp(step), ws.data_ptr(), need, _stream()))
+    increment_version(params)
+    if masters is not None:
+        increment_version(masters)
 
 
 def adamw_moments(exp_avgs, exp_avg_sqs, exp_avg_scales, exp_avg_sq_scales, out=None):
@@ -396,6 +406,8 @@ def adamw_moments(exp_avgs, exp_avg_sqs, exp_avg_scales, exp_avg_sq_scales, out=
     to = [(ctypes.c_uint64 * max(count, 1))(*_column(o, count, "out", torch.float32, sizes)) for o in out]
     array = _descriptors(count, (None, None, *columns[:2], None, *columns[2:], sizes))
     _check(lib().rsc_adamw_moments(array, count, to[0], to[1], _stream()))
+    for tensors in out:
+        increment_version(tensors)
     return out
 
 

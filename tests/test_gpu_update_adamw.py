@@ -335,3 +335,38 @@ def test_more_than_2_to_31_elements():
     assert same(host(m[first:]), want[1]) and same(host(v[first:]), want[2])
     assert same(host(ms[first // 256:]), want[3]) and same(host(vs[first // 256:]), want[4])
     assert int(step) == 4
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_is_a_write_in_place_to_autograd(bits, dtype):
+    """A graph that saved a weight before the step must not go on with the new
+    one: as after torch's optimizers its backward pass raises."""
+    w = torch.nn.Parameter(torch.randn((16, 24), device="cuda").to(dtype))
+    other = torch.nn.Parameter(torch.randn((16, 24), device="cuda").to(dtype))
+    opt = rsc.AdamW([w], state_bits=bits)
+    x = torch.randn((5, 16), device="cuda").to(dtype).requires_grad_()
+    for product in (lambda: x @ w, lambda: rsc.linear(x, w), lambda: rsc.linear_cross_entropy(
+            x, w, torch.zeros(5, dtype=torch.int64, device="cuda"))):
+        y, untouched = product(), x @ other
+        w.grad = torch.ones_like(w)
+        opt.step()
+        with pytest.raises(RuntimeError, match="inplace"):
+            torch.autograd.grad(y.sum(), x)
+        torch.autograd.grad(untouched.sum(), x)
+        torch.autograd.grad(product().sum(), x)
+    s = make([300], dtype, bits, True, 1)
+    a = torch.ones(300, device="cuda", requires_grad=True)
+    on = [(s["p"][0] * a).sum(), (s["w"][0] * a).sum()]
+    rsc.adamw_step(s["p"], s["g"], s["m"], s["v"], torch.zeros(1, dtype=torch.int64, device="cuda"), masters=s["w"],
+                   exp_avg_scales=s["ms"], exp_avg_sq_scales=s["vs"])
+    for y in on:
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.backward()
+    if bits == 8:
+        out = [torch.ones(300, device="cuda")], [torch.ones(300, device="cuda")]
+        on = [(t[0] * a).sum() for t in out]
+        rsc.adamw_moments(s["m"], s["v"], s["ms"], s["vs"], out=out)
+        for y in on:
+            with pytest.raises(RuntimeError, match="inplace"):
+                y.backward()

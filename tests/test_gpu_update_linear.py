@@ -397,3 +397,26 @@ def test_relu_masks_beside_rows_of_another_scale(size, dtype):
     z = exact + b.double()
     assert bool((z[row, column].abs() <= 2.0 ** -24 * exact[row, column].abs()).all())
     assert torch.equal(y > 0, z > 0)
+
+
+def test_out_is_a_write_in_place_to_autograd():
+    """A backward pass that saved `out`'s old values raises, and a tensor that
+    requires gradients is no place for a result without them."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x, w = rand((9, 16), torch.float32, g), rand((16, 24), torch.float32, g)
+    buffer, a = rand((9, 24), torch.float32, g), torch.ones((9, 24), device="cuda", requires_grad=True)
+    y = (buffer * a).sum()
+    rsc.linear(x, w, out=buffer)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
+    (buffer * a).sum().backward()
+    assert torch.equal(a.grad, rsc.linear(x, w))
+    for out in (a, a * 2):
+        with pytest.raises(ValueError):
+            rsc.linear(x, w, out=out)
+    with torch.no_grad():
+        rsc.linear(x, w, out=a)
+    assert torch.equal(a.detach(), buffer)
+    with torch.inference_mode():
+        held = torch.empty((9, 24), device="cuda")
+        assert torch.equal(rsc.linear(x, w, out=held), buffer)
