@@ -31,11 +31,11 @@ _REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
 # (small calls are bound by the host's time for them, so each property is read
 # from a tensor once)
 def _new(rows: int, cols: int, dtype, device) -> torch.Tensor:
-    """rows x cols view of rows that are whole 16-byte units."""
+    """rows x cols, in rows that are whole 16-byte units. No view of a wider
+    tensor: autograd refuses writes in place to views that a Function returns."""
     u = 16 // dtype.itemsize
     ld = (cols + u - 1) // u * u
-    t = torch.empty((rows, ld), dtype=dtype, device=device)
-    return t if ld == cols else t[:, :cols]
+    return torch.empty_strided((rows, cols), (ld, 1), dtype=dtype, device=device)
 
 
 def _ld(t: torch.Tensor) -> int | None:
@@ -79,11 +79,9 @@ def _weights(w: torch.Tensor) -> tuple[torch.Tensor, int, int]:
 
 def _new_like_weights(w: torch.Tensor, out_major: int) -> tuple[torch.Tensor, int]:
     k, m = w.shape
-    if out_major:
-        t = _new(m, k, w.dtype, w.device)
-        return t.t(), _ld(t)
-    t = _new(k, m, w.dtype, w.device)
-    return t, _ld(t)
+    u = 16 // w.dtype.itemsize
+    ld = ((k if out_major else m) + u - 1) // u * u
+    return torch.empty_strided((k, m), (1, ld) if out_major else (ld, 1), dtype=w.dtype, device=w.device), ld
 
 
 def _check_operand(t: torch.Tensor, name: str, shape, dtype=None) -> None:
@@ -200,8 +198,9 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = No
 
     x [n, k], weight [k, m] in either storage order (a transposed view of an
     [m, k] tensor is used as it lies), residual [n, m], all of one type;
-    bias [m] of that type or float32. Differentiable once in all four; dW has
-    weight's storage order. With gradients a ReLU's sign next to zero is decided
+    bias [m] of that type or float32. The result's rows are whole 16-byte units
+    apart, so with other m it is not contiguous (reshape, not view, flattens it).
+    Differentiable once in all four; dW has weight's storage order. With gradients a ReLU's sign next to zero is decided
     in 64 bits (at most 32 times in some thousand results), and GELU and SiLU
     keep their argument, n x m float32. out (no gradients): [n, m] with aligned rows, may
     be the residual; the write counts as one in place to autograd."""

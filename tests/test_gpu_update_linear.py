@@ -420,3 +420,36 @@ def test_out_is_a_write_in_place_to_autograd():
     with torch.inference_mode():
         held = torch.empty((9, 24), device="cuda")
         assert torch.equal(rsc.linear(x, w, out=held), buffer)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [40, 41, 1])
+@pytest.mark.parametrize("n", [50, 1])
+def test_results_can_be_changed_in_place(n, m, dtype):
+    """With whole and with ragged rows, results and gradients alike; a ReLU's
+    result is what its backward pass reads, so that one raises."""
+    x, w, b, _, dy = inputs(n, 24, m, dtype, False, 14)
+    x2, w2 = x.clone(), w.clone()
+    for t in (x, w, b):
+        t.requires_grad_()
+    y = rsc.linear(x, w, b, act="gelu")
+    want = torch.autograd.grad(y, [x, w, b], 2 * dy)
+    y = rsc.linear(x, w, b, act="gelu")
+    before = y.detach().clone()
+    y.mul_(2).add_(1)
+    assert torch.equal(y.detach(), 2 * before + 1) and not y.is_leaf
+    got = torch.autograd.grad(y, [x, w, b], dy)
+    for p, q in zip(got, want):
+        assert torch.equal(p, q) and not p._is_view()
+        p.mul_(2)
+        assert torch.equal(p, 2 * q)
+    y = rsc.linear(x, w, b, act="relu")
+    y.mul_(2)
+    with pytest.raises(RuntimeError, match="inplace"):
+        torch.autograd.grad(y, x, dy)
+    # the weights' gradient in the order of weights stored the other way
+    w3 = w2.t().contiguous().t().requires_grad_()
+    g, = torch.autograd.grad(rsc.linear(x2, w3), w3, dy)
+    assert not g._is_view() and (g.stride(0) == 1 or m == 1)
+    y = rsc.linear(x2, w2)      # (without gradients)
+    y.mul_(2)
