@@ -411,7 +411,7 @@ def adamw_moments(exp_avgs, exp_avg_sqs, exp_avg_scales, exp_avg_sq_scales, out=
 
 
 class AdamW(torch.optim.Optimizer):
-    """AdamW (decoupled weight decay) over the library's one-launch step.
+    """AdamW (decoupled weight decay) over the library's step of many tensors.
 
     state_bits: 32 (float32 moments) or 8 (codes with a scale for each 256
     elements: 2.03 bytes a parameter instead of 8). 16-bit parameters keep
@@ -421,8 +421,16 @@ class AdamW(torch.optim.Optimizer):
 
     The state of a parameter is made at its first step, which can therefore
     not be captured into a HIP graph; later ones can (a captured step holds
-    lr, betas, eps and weight_decay of its capture). Each parameter group
-    counts its own steps."""
+    lr, betas, eps and weight_decay of its capture).
+
+    Each parameter's steps are counted, as torch's optimizer does: bias
+    corrections of one whose gradients come later, or not in every step, are its
+    own. Parameters that have taken the same steps share a count on the device
+    and one call (group["counts"], group["count_of"]); a step in which only some of
+    them have gradients gives these a count of their own, which cannot happen
+    in a capture nor, since a captured step holds its counts, after one: run such
+    a step once before. group["step"] counts the steps of the group (while it has
+    more than one count, without those of graphs from before)."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
                  state_bits: int = 32, master_weights: bool = True, seed: int = 0):
@@ -453,32 +461,73 @@ class AdamW(torch.optim.Optimizer):
                 s["master"] = p.detach().float()
         return s
 
+    def _parts(self, group, used: list[int]) -> list[tuple[int, list[int]]]:
+        """The parameters `used` by their counts: (number of the count, which of
+        the group's parameters)."""
+        params, capturing = group["params"], torch.cuda.is_current_stream_capturing()
+        captured = self.__dict__.setdefault("_captured", [])    # counts that a graph holds
+        if "counts" not in group:
+            # (a state that counts by group only: its parameters go on from there)
+            group["counts"] = [group["step"]] if "step" in group else []
+            group["count_of"] = [0 if "step" in group and self.state.get(p) else -1 for p in params]
+        counts, of = group["counts"], group["count_of"]
+        of.extend([-1] * (len(params) - len(of)))
+        by_count: dict[int, list[int]] = {}
+        for i in used:
+            by_count.setdefault(of[i], []).append(i)
+        parts = []
+        for count, members in by_count.items():
+            if count < 0 or len(members) < of.count(count):
+                if capturing or (count >= 0 and any(t is counts[count] for t in captured)):
+                    raise RuntimeError("the first step with gradients for just these parameters makes their count: it "
+                                       "cannot be captured, nor come after a captured step of them")
+                counts.append(torch.zeros(1, dtype=torch.int64, device=params[members[0]].device) if count < 0
+                              else counts[count].clone())
+                count = len(counts) - 1
+                for i in members:
+                    of[i] = count
+            parts.append((count, members))
+        group.setdefault("step", counts[0])
+        if capturing:
+            captured.extend(counts[count] for count, _ in parts)
+        return parts
+
+    def _step_of(self, group, used: list[torch.Tensor], count: torch.Tensor) -> None:
+        states = [self.state[p] for p in used]
+        bits8 = group["state_bits"] == 8
+        adamw_step([p.detach() for p in used], [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in used],
+                   [s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states], count,
+                   lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
+                   masters=[s["master"] for s in states] if "master" in states[0] else None,
+                   exp_avg_scales=[s["exp_avg_scale"] for s in states] if bits8 else None,
+                   exp_avg_sq_scales=[s["exp_avg_sq_scale"] for s in states] if bits8 else None,
+                   seed=group["seed"])
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        todo = []      # (every group is checked before the first one's step)
         for group in self.param_groups:
-            used = [p for p in group["params"] if p.grad is not None]
+            params = group["params"]
+            used = [i for i, p in enumerate(params) if p.grad is not None]
             if not used:
                 continue
-            if "step" not in group:
-                if torch.cuda.is_current_stream_capturing():
-                    raise RuntimeError("the first step cannot be captured")
-                group["step"] = torch.zeros(1, dtype=torch.int64, device=used[0].device)
-            types = sorted({p.dtype for p in used}, key=str)
+            types = sorted({params[i].dtype for i in used}, key=str)
             if len(types) > 1:
                 raise ValueError(f"a parameter group holds {types}: one type a group")
-            states = [self._state_of(p, group) for p in used]
-            bits8 = group["state_bits"] == 8
-            adamw_step([p.detach() for p in used], [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in used],
-                       [s["exp_avg"] for s in states], [s["exp_avg_sq"] for s in states], group["step"],
-                       lr=group["lr"], betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"],
-                       masters=[s["master"] for s in states] if "master" in states[0] else None,
-                       exp_avg_scales=[s["exp_avg_scale"] for s in states] if bits8 else None,
-                       exp_avg_sq_scales=[s["exp_avg_sq_scale"] for s in states] if bits8 else None,
-                       seed=group["seed"])
+            todo.append((group, self._parts(group, used)))
+            for i in used:
+                self._state_of(params[i], group)
+        for group, parts in todo:
+            if len(group["counts"]) > 1:   # (a single count is the group's, too)
+                if group["step"] is group["counts"][0]:
+                    group["step"] = group["step"].clone()
+                group["step"].add_(1)
+            for count, members in parts:
+                self._step_of(group, [group["params"][i] for i in members], group["counts"][count])
         return loss
 
     def load_state_dict(self, state_dict) -> None:
@@ -491,4 +540,11 @@ class AdamW(torch.optim.Optimizer):
                     self.state[p] = {name: v.detach().to(p.device, copy=True) if isinstance(v, torch.Tensor) else v
                                      for name, v in state_dict["state"][key].items()}
             if isinstance(group.get("step"), torch.Tensor) and group["params"]:
-                group["step"] = saved["step"].detach().to(group["params"][0].device, copy=True)
+                device = group["params"][0].device
+                # (none in a state that was saved when steps were counted by group only)
+                if "counts" in saved:
+                    group["counts"] = [t.detach().to(device, copy=True) for t in saved["counts"]]
+                    group["count_of"] = list(saved["count_of"])
+                group["step"] = group["counts"][0] if len(saved.get("counts", ())) == 1 \
+                    else saved["step"].detach().to(device, copy=True)
+        self.__dict__["_captured"] = []

@@ -370,3 +370,118 @@ def test_a_step_is_a_write_in_place_to_autograd(bits, dtype):
         for y in on:
             with pytest.raises(RuntimeError, match="inplace"):
                 y.backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_late_and_resting_parameters_are_those_of_torch(dtype):
+    """Gradients from the sixth step on, in every third step and in every step:
+    each parameter's bias corrections go by its own steps."""
+    g = torch.Generator().manual_seed(0)
+    ps = [torch.nn.Parameter(torch.randn(500, generator=g).to(dtype).cuda()) for _ in range(5)]
+    qs = [torch.nn.Parameter(p.detach().float()) for p in ps]
+    a, b = rsc.AdamW(ps, lr=1e-2, weight_decay=0.1), torch.optim.AdamW(qs, lr=1e-2, weight_decay=0.1)
+    when = [lambda i: True, lambda i: i >= 5, lambda i: i >= 5, lambda i: i % 3 == 0, lambda i: i >= 9 or i == 2]
+    for i in range(20):
+        for p, q, on in zip(ps, qs, when):
+            p.grad = torch.sin(q.detach() * (i + 1)).to(dtype) if on(i) else None
+            q.grad = p.grad.float() if on(i) else None
+        a.step()
+        b.step()
+    for p, q in zip(ps, qs):
+        # 20 steps of at most lr (1 + small) each, every one with fewer than 16 roundings
+        p, q = a.state[p]["master"] if dtype == torch.bfloat16 else p.detach(), q.detach()
+        assert float((p - q).abs().max()) <= 20 * 16 * 2.0 ** -24 * (float(q.abs().max()) + 0.2)
+    group = a.param_groups[0]
+    assert [int(group["counts"][c]) for c in group["count_of"]] == [20, 15, 15, 7, 12] and int(group["step"]) == 20
+    assert group["count_of"][1] == group["count_of"][2]     # one call for both
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_counts_go_through_a_saved_state(bits, tmp_path):
+    def build():
+        g = torch.Generator().manual_seed(0)
+        ps = [torch.nn.Parameter(torch.randn(n, generator=g).cuda()) for n in (300, 4097, 5)]
+        return ps, rsc.AdamW(ps, lr=1e-2, state_bits=bits, seed=3)
+
+    def go(ps, opt, i):
+        for j, p in enumerate(ps):
+            p.grad = torch.full_like(p, 0.1 * (i + 1)) * p.detach() if j == 0 or i > 2 or (j == 1 and i == 1) else None
+        opt.step()
+
+    for steps in (1, 5):     # one count, three of them
+        ps, opt = build()
+        for i in range(steps):
+            go(ps, opt, i)
+        torch.save(opt.state_dict(), tmp_path / "state")
+        qs, opt2 = build()
+        with torch.no_grad():
+            for p, q in zip(ps, qs):
+                q.copy_(p)
+        opt2.load_state_dict(torch.load(tmp_path / "state", map_location="cpu", weights_only=True))
+        for i in range(steps, steps + 3):
+            go(ps, opt, i)
+            go(qs, opt2, i)
+        assert all(torch.equal(p, q) for p, q in zip(ps, qs))
+        for x, y in zip(opt.param_groups, opt2.param_groups):
+            assert x["count_of"] == y["count_of"] and [int(c) for c in x["counts"]] == [int(c) for c in y["counts"]]
+            assert int(x["step"]) == int(y["step"]) == steps + 3
+    # a state that counts by group only goes on from that count
+    ps, opt = build()
+    for i in range(3, 6):
+        go(ps, opt, i)
+    saved = opt.state_dict()
+    for group in saved["param_groups"]:
+        del group["counts"], group["count_of"]
+    qs, opt2 = build()
+    with torch.no_grad():
+        for p, q in zip(ps, qs):
+            q.copy_(p)
+    opt2.load_state_dict(saved)
+    go(ps, opt, 6)
+    go(qs, opt2, 6)
+    assert all(torch.equal(p, q) for p, q in zip(ps, qs))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_steps_keep_their_counts(bits):
+    """A captured step of parameters with different counts advances each; what
+    would part the counts that a graph holds is refused."""
+    def build():
+        g = torch.Generator().manual_seed(0)
+        ps = [torch.nn.Parameter(torch.randn(n, generator=g).cuda()) for n in (300, 700, 20, 10)]
+        return ps, rsc.AdamW(ps, lr=1e-2, state_bits=bits)
+
+    def grads(ps, live):
+        for j, p in enumerate(ps):
+            p.grad = torch.full_like(p, 0.01 * (j + 1)) if j in live else None
+
+    (ps, opt), (qs, other) = build(), build()
+    for live in ((0, 1), (0, 1, 2), (0, 1, 2)):
+        for a, o in ((ps, opt), (qs, other)):
+            grads(a, live)
+            o.step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        other.step()
+        assert all(torch.equal(p, q) for p, q in zip(ps, qs))
+    grads(ps, (0, 2))
+    before = [p.detach().clone() for p in ps]
+    with pytest.raises(RuntimeError, match="count"):
+        opt.step()
+    assert all(torch.equal(p, q) for p, q in zip(ps, before))
+    for a, o in ((ps, opt), (qs, other)):
+        grads(a, (2, 3))       # one more parameter begins
+        o.step()
+        grads(a, (0, 1, 2, 3))
+        o.step()
+    assert all(torch.equal(p, q) for p, q in zip(ps, qs))
+    group = opt.param_groups[0]
+    assert [int(group["counts"][c]) for c in group["count_of"]] == [7, 7, 7, 2]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert [int(group["counts"][c]) for c in group["count_of"]] == [8, 8, 8, 2]
