@@ -410,6 +410,20 @@ def adamw_moments(exp_avgs, exp_avg_sqs, exp_avg_scales, exp_avg_sq_scales, out=
     return out
 
 
+def _seed_of(seed: int, group: int, count: int) -> int:
+    """Each call of a step draws words of its own (a call numbers its elements
+    from 0): the seed itself for the first group's first count, for the others an output
+    of SplitMix64 (Steele, Lea and Flood 2014) seeded with it."""
+    number = (group << 32) + count
+    if number == 0:
+        return seed
+    mask = (1 << 64) - 1
+    z = (seed + number * 0x9E3779B97F4A7C15) & mask
+    z = ((z ^ (z >> 30)) * 0xBF58476D1CE4E5B9) & mask
+    z = ((z ^ (z >> 27)) * 0x94D049BB133111EB) & mask
+    return z ^ (z >> 31)
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW (decoupled weight decay) over the library's step of many tensors.
 
@@ -492,7 +506,7 @@ class AdamW(torch.optim.Optimizer):
             captured.extend(counts[count] for count, _ in parts)
         return parts
 
-    def _step_of(self, group, used: list[torch.Tensor], count: torch.Tensor) -> None:
+    def _step_of(self, group, used: list[torch.Tensor], count: torch.Tensor, seed: int) -> None:
         states = [self.state[p] for p in used]
         bits8 = group["state_bits"] == 8
         adamw_step([p.detach() for p in used], [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in used],
@@ -501,7 +515,7 @@ class AdamW(torch.optim.Optimizer):
                    masters=[s["master"] for s in states] if "master" in states[0] else None,
                    exp_avg_scales=[s["exp_avg_scale"] for s in states] if bits8 else None,
                    exp_avg_sq_scales=[s["exp_avg_sq_scale"] for s in states] if bits8 else None,
-                   seed=group["seed"])
+                   seed=seed)
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -510,7 +524,7 @@ class AdamW(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         todo = []      # (every group is checked before the first one's step)
-        for group in self.param_groups:
+        for number, group in enumerate(self.param_groups):
             params = group["params"]
             used = [i for i, p in enumerate(params) if p.grad is not None]
             if not used:
@@ -518,16 +532,17 @@ class AdamW(torch.optim.Optimizer):
             types = sorted({params[i].dtype for i in used}, key=str)
             if len(types) > 1:
                 raise ValueError(f"a parameter group holds {types}: one type a group")
-            todo.append((group, self._parts(group, used)))
+            todo.append((number, group, self._parts(group, used)))
             for i in used:
                 self._state_of(params[i], group)
-        for group, parts in todo:
+        for number, group, parts in todo:
             if len(group["counts"]) > 1:   # (a single count is the group's, too)
                 if group["step"] is group["counts"][0]:
                     group["step"] = group["step"].clone()
                 group["step"].add_(1)
             for count, members in parts:
-                self._step_of(group, [group["params"][i] for i in members], group["counts"][count])
+                self._step_of(group, [group["params"][i] for i in members], group["counts"][count],
+                              _seed_of(group["seed"], number, count))
         return loss
 
     def load_state_dict(self, state_dict) -> None:

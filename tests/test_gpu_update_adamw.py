@@ -485,3 +485,28 @@ def test_captured_steps_keep_their_counts(bits):
     graph.replay()
     torch.cuda.synchronize()
     assert [int(group["counts"][c]) for c in group["count_of"]] == [8, 8, 8, 2]
+
+
+def test_groups_draw_their_own_words():
+    """Equal parameters in different groups, or with different counts, round
+    their codes independently; the first group's are those of the seed."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    value = torch.randn(5000, generator=g, device="cuda")
+    grads = [torch.randn(5000, generator=g, device="cuda") for _ in range(4)]
+    ps = [torch.nn.Parameter(value.clone()) for _ in range(4)]
+    opt = rsc.AdamW([{"params": ps[:2]}, {"params": ps[2:]}], state_bits=8, seed=5)
+    for i, gr in enumerate(grads[:3]):
+        for j, p in enumerate(ps):
+            p.grad = gr.clone() if j != 1 or i else None     # (the second one begins a step later)
+        opt.step()
+    alone = rsc.AdamW([torch.nn.Parameter(value.clone())], state_bits=8, seed=5)
+    for gr in grads[:3]:
+        alone.param_groups[0]["params"][0].grad = gr.clone()
+        alone.step()
+    codes = [opt.state[p]["exp_avg"].int() for p in ps]
+    assert torch.equal(codes[0], alone.state[alone.param_groups[0]["params"][0]]["exp_avg"].int())
+    # a code is rounded up or down by its draw: two draws of a uniform remainder
+    # differ for a third of the elements
+    for a, b in ((0, 2), (1, 2), (2, 3)):
+        differ = float((codes[a] != codes[b]).float().mean())
+        assert differ > 0.2, (a, b, differ)
