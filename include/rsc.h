@@ -601,7 +601,9 @@ rsc_status_t rsc_xent(const rsc_xent_t *p, const void *X, int64_t ldx, const voi
                       const void *targets, float *loss, float *lse, float *count, void *G, int64_t ldg, void *ws,
                       size_t ws_bytes, hipStream_t stream);
 /* Gradients for dloss (device, fp32; 1 value, or n with reduction 0): dX (n x
- * k), dW (stored as W is) and dbias, each may be NULL. G: what rsc_xent wrote
+ * k), dW (stored as W is) and dbias, each may be NULL. The logits' gradient is
+ * held in the operands' type for dX and dW; dbias sums it from before that
+ * rounding, except with G. G: what rsc_xent wrote
  * there for the same arguments, or NULL: the logits are then formed again. The
  * workspace holds one piece of the logits' gradient (256 MiB, or n x 2,048
  * values where that is more; none with G) and, with more than one piece, dX in

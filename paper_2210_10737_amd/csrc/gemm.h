@@ -1204,7 +1204,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
     __shared__ __attribute__((aligned(1024))) char lds[G::LDS];
     const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     const Place o = place(tm, tn, 1);
-    static_assert(G::THREADS >= BM, "a row each");
+    static_assert(G::THREADS >= BM && G::THREADS >= BN, "a row and a column each");
     const int tid = threadIdx.x;
     // a row's class, factor and log-sum-exp, on their way while the logits are formed
     int64_t own_class = -1;
@@ -1231,6 +1231,10 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
     const Spot at = spot_of<G, W>(p, o.m * BM, o.n * BN);
     float bias[W];
     load_bias<T>(c.bias, c.bias_f32, at.n, at.count, bias);
+    // the columns' sums, from before G is rounded (fp32: 19 additions to a lane's
+    // rows and its neighbours', the rest in 64 bits)
+    using Sum = std::conditional_t<sizeof(T) == 4, double, float>;
+    Sum column[W] = {};
     by_rows<G, W>(acc, lds, [&](int down, float (&v)[W]) {
         const int m = at.m + down;
         if (m >= p.m || at.count <= 0) return;
@@ -1243,8 +1247,32 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
             for (int i = 0; i < W; ++i)
                 if (i == own) v[i] -= row.weight;
         }
+        if (c.sums) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) column[i] += (Sum)v[i];
+        }
         store_row((T *)c.grad + (at.m * c.ldgrad + at.n) + down * c.ldgrad, at.count, v);
     });
+    if (!c.sums) return;
+    // over the lanes that hold other rows of the same columns, then over the waves
+    constexpr int LANES = G::TB * 32 / W;
+    const int wave = tid >> 6, lane = tid & 63;
+    Sum *const part = (Sum *)(lds + SLABS + BM * sizeof(Row));
+    static_assert(SLABS + BM * (int)sizeof(Row) + C::WM * BN * (int)sizeof(Sum) <= G::LDS, "and the waves' sums");
+    static_assert((SLABS + BM * sizeof(Row)) % sizeof(Sum) == 0, "aligned");
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+#pragma unroll
+        for (int d = LANES; d < 64; d *= 2) column[i] += __shfl_xor(column[i], d);
+        if (lane < LANES) part[(wave / C::WN) * BN + (wave % C::WN) * G::TB * 32 + lane * W + i] = column[i];
+    }
+    __syncthreads();
+    if (tid < BN && o.n * BN + tid < p.n) {
+        double sum = 0.0;
+#pragma unroll
+        for (int w = 0; w < C::WM; ++w) sum += (double)part[w * BN + tid];
+        c.sums[(int64_t)o.m * p.n + o.n * BN + tid] = sum;
+    }
 }
 
 }  // namespace gemm

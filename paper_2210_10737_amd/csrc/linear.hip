@@ -221,8 +221,10 @@ hipError_t pass_launch(int32_t dtype, Pass p, const Chunks &c, hipStream_t strea
     return hipGetLastError();
 }
 
-hipError_t total_launch(int32_t dtype, const double *part, int32_t chunks, int32_t m, float scale,
-                        const float *scale_dev, void *out, int32_t out_f32, hipStream_t stream) {
+}  // namespace
+
+hipError_t column_total_launch(int32_t dtype, const double *part, int32_t chunks, int32_t m, float scale,
+                               const float *scale_dev, void *out, int32_t out_f32, hipStream_t stream) {
     const unsigned grid = (unsigned)ceil_div(m, 16);
     if (dtype == kF32 || out_f32)
         column_total_kernel<float><<<grid, 1024, 0, stream>>>(part, chunks, m, scale, scale_dev, (float *)out);
@@ -232,8 +234,6 @@ hipError_t total_launch(int32_t dtype, const double *part, int32_t chunks, int32
         column_total_kernel<_Float16><<<grid, 1024, 0, stream>>>(part, chunks, m, scale, scale_dev, (_Float16 *)out);
     return hipGetLastError();
 }
-
-}  // namespace
 
 hipError_t zero_launch(int32_t dtype, void *p, int64_t ld, int64_t rows, int64_t cols, hipStream_t stream) {
     if (rows <= 0 || cols <= 0) return hipSuccess;
@@ -390,7 +390,7 @@ hipError_t column_sum_launch(int32_t dtype, const void *a, int64_t lda, int64_t 
     p.n = n;
     p.m = (int32_t)m;
     hipError_t e = pass_launch(dtype, p, c, stream);
-    if (e == hipSuccess) e = total_launch(dtype, p.part, c.count, (int32_t)m, scale, scale_dev, out, out_f32, stream);
+    if (e == hipSuccess) e = column_total_launch(dtype, p.part, c.count, (int32_t)m, scale, scale_dev, out, out_f32, stream);
     return e;
 }
 
@@ -436,7 +436,7 @@ hipError_t linear_backward_launch(const Linear &l, const void *dy, int64_t lddy,
         const Chunks c = chunks_of(l.dtype, l.n, l.m);
         e = pass_launch(l.dtype, p, c, stream);
         if (g.db && e == hipSuccess)
-            e = total_launch(l.dtype, part, c.count, l.m, 1.f, nullptr, g.db, g.db_f32, stream);
+            e = column_total_launch(l.dtype, part, c.count, l.m, 1.f, nullptr, g.db, g.db_f32, stream);
     }
     if (g.dx && e == hipSuccess) {
         // dX = alpha dZ W^T

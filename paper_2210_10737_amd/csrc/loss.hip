@@ -6,8 +6,9 @@
 // row by row into lse = log sum exp, and loss = lse - own logit.
 // Backward: the classes are taken in pieces; each piece's logits are computed
 // again and leave as G = weight (exp(logit - lse) - [own class]) in the
-// operands' type, from which dX += G W^T, dW = X^T G and db = sum G of the
-// piece follow. Only one piece of G is ever held.
+// operands' type, from which dX += G W^T and dW = X^T G of the piece follow, and
+// as its columns' sums from before that rounding, for db. Only one piece of G is
+// ever held.
 //
 // G has no small factors in it (1/count, the upstream gradient): those go into
 // the products' fp32 epilogues. fp16's G is scaled by 2^10 as well, so that
@@ -249,13 +250,23 @@ size_t piece_cuts(const Loss &l, bool dx, bool dw) {
     }
     return align_up(b, 256);
 }
+// the columns' partial sums: of each row of tiles where the gradient pass forms
+// G, of column_sum_launch's chunks where G is given
+size_t sums_bytes(const Loss &l, bool kept) {
+    const int64_t piece = piece_of(l), rest = l.v % piece;
+    if (kept) return column_sum_ws_bytes(l.n, piece);
+    size_t b = 0;
+    for (int64_t v : {piece, rest})
+        if (v > 0) b = std::max(b, sizeof(double) * (size_t)(v * ceil_div(l.n, kShapes[loss_shape(l.dtype, l.n, v, l.k)].bm)));
+    return align_up(b, 256);
+}
 int64_t grad_ld(const Loss &l) { return (int64_t)align_up((size_t)piece_of(l), 16 / value_size(l.dtype)); }
 int64_t acc_ld(const Loss &l) { return (int64_t)align_up((size_t)l.k, 4); }
 }  // namespace
 
 size_t loss_backward_ws_bytes(const Loss &l, bool dx, bool dw, bool kept) {
     if (l.n == 0) return 256;
-    size_t b = 256 + column_sum_ws_bytes(l.n, piece_of(l)) + piece_cuts(l, dx, dw);
+    size_t b = 256 + sums_bytes(l, kept) + piece_cuts(l, dx, dw);
     if (!kept)
         b += align_up((size_t)l.n * grad_ld(l) * value_size(l.dtype), 256) + align_up(sizeof(float) * (size_t)l.n, 256);
     if (dx && piece_of(l) < l.v) b += align_up(sizeof(float) * (size_t)l.n * acc_ld(l), 256);
@@ -285,7 +296,7 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
     float *factor = (float *)at;
     at += 256;
     void *sums = at;
-    at += column_sum_ws_bytes(l.n, piece);
+    at += sums_bytes(l, kept);
     float *acc = nullptr;
     if (g.dx && piece < l.v) {
         acc = (float *)at;
@@ -299,6 +310,7 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
     e = hipGetLastError();
     c.weight = weight;
     c.scale = grad_scale(l);
+    c.sums = g.db && !kept ? (double *)sums : nullptr;
     const void *bias = c.bias;
     for (int64_t v0 = 0; v0 < l.v && e == hipSuccess; v0 += piece) {
         const int32_t vc = (int32_t)std::min(piece, l.v - v0);
@@ -313,7 +325,8 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
         p.m = l.n;
         p.n = vc;
         p.k = l.k;
-        if (!kept) e = grad_fn(l)(loss_shape(l.dtype, l.n, vc, l.k), p, c, stream);
+        const int shape = loss_shape(l.dtype, l.n, vc, l.k);
+        if (!kept) e = grad_fn(l)(shape, p, c, stream);
         if (g.dx && e == hipSuccess) {
             Product q;
             q.a = c.grad;
@@ -353,9 +366,14 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
             o.ldy = g.lddw;
             e = product_launch(l.dtype, kColsCols, q, o, cut, stream);
         }
-        if (g.db && e == hipSuccess)
-            e = column_sum_launch(l.dtype, c.grad, c.ldgrad, l.n, vc, 1.f / c.scale, factor,
-                                  (char *)g.db + v0 * (g.db_f32 ? 4 : es), g.db_f32, sums, stream);
+        if (g.db && e == hipSuccess) {
+            void *const db = (char *)g.db + v0 * (g.db_f32 ? 4 : es);
+            if (kept)
+                e = column_sum_launch(l.dtype, c.grad, c.ldgrad, l.n, vc, 1.f / c.scale, factor, db, g.db_f32, sums, stream);
+            else
+                e = column_total_launch(l.dtype, c.sums, (int32_t)ceil_div(l.n, kShapes[shape].bm), vc, 1.f / c.scale,
+                                        factor, db, g.db_f32, stream);
+        }
     }
     return e;
 }

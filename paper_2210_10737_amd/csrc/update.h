@@ -62,6 +62,7 @@ struct Classes {
     int64_t first = 0;  // the piece's first class
     void *grad = nullptr;
     int64_t ldgrad = 0;
+    double *sums = nullptr;  // gradient pass, nullable: each row of tiles' column sums, the piece's width apart
 
     __device__ __forceinline__ int64_t raw(int m) const {
         return targets_i32 ? (int64_t)((const int32_t *)targets)[m] : ((const int64_t *)targets)[m];
@@ -129,6 +130,9 @@ hipError_t linear_backward_launch(const Linear &l, const void *dy, int64_t lddy,
                                   void *ws, hipStream_t stream);
 // out[j] = scale * scale_dev * sum over rows of a[i][j] (fp32 sums in one fixed order); scale_dev nullable
 size_t column_sum_ws_bytes(int64_t n, int64_t m);
+// out[j] = scale * scale_dev * the sum of part[i * m + j] over the chunks
+hipError_t column_total_launch(int32_t dtype, const double *part, int32_t chunks, int32_t m, float scale,
+                               const float *scale_dev, void *out, int32_t out_f32, hipStream_t stream);
 hipError_t zero_launch(int32_t dtype, void *p, int64_t ld, int64_t rows, int64_t cols, hipStream_t stream);
 hipError_t column_sum_launch(int32_t dtype, const void *a, int64_t lda, int64_t n, int64_t m, float scale,
                              const float *scale_dev, void *out, int32_t out_f32, void *ws, hipStream_t stream);

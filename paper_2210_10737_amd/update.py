@@ -256,7 +256,9 @@ def _xent_forward(x, weight, targets, bias, ignore_index: int, reduction: int, k
 class _Xent(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, targets, bias, ignore_index, reduction):
-        loss, kept, grad, xa, wa = _xent_forward(x, weight, targets, bias, ignore_index, reduction, True)
+        # (kept, G is in the operands' type: a float32 bias's gradient comes from before that rounding)
+        keep = bias is None or bias.dtype == x.dtype or not ctx.needs_input_grad[3]
+        loss, kept, grad, xa, wa = _xent_forward(x, weight, targets, bias, ignore_index, reduction, keep)
         ctx.save_for_backward(xa, wa, targets, bias, kept, grad)
         ctx.options = (ignore_index, reduction)
         return loss

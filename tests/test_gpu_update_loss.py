@@ -293,3 +293,33 @@ def test_long_ranges_of_classes_at_the_lowest_value(v, masked, lowest, dtype):
     want, off = grad.sum(0), grad_off.sum(0)
     close(got[2][rest], want, off + half(b.dtype) * (want.abs() + off) + small, "db")
     assert not got[1][:, masked[0]:masked[1]].any() and not got[2][masked[0]:masked[1]].any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("reduction", ["mean", "none"])
+@pytest.mark.parametrize("size", [(70, 48, 300), (150, 48, 41), (257, 64, 1500), (4000, 24, 300), (66000, 16, 2300), (1, 8, 2)])
+def test_an_fp32_bias_gets_its_gradient_from_unrounded_values(size, reduction, dtype):
+    """The logits' gradient is held in the operands' type for the products; the
+    bias's sums are formed before that rounding. A probability is off by its
+    logit and its row's lse (`row_off` each) and by two exponentials and a sum of at
+    most 130 positive terms, arguments up to 32: (64 + 130 + 8) 2^-24 < 2^-16; the
+    sum over rows by fewer than 32 roundings of 2^-24, the result by one."""
+    n, k, v = size
+    x, w, b, t = inputs(n, k, v, dtype, True, 0.8, 31)
+    b = b.float().requires_grad_()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    up = torch.randn(n, generator=g, device="cuda") if reduction == "none" else torch.full((), 1.5, device="cuda")
+    for leaves in ((b,), (b, x, w)):
+        for a in (x, w):
+            a.requires_grad_(len(leaves) > 1)
+        got = torch.autograd.grad(rsc.linear_cross_entropy(x, w, t, b, reduction=reduction), leaves, up)[0]
+        x6, w6 = x.detach().double(), w.detach().double()
+        z, mag = x6 @ w6 + b.detach().double(), x6.abs() @ w6.abs() + b.detach().double().abs()
+        row_off = (sums(k) * mag).amax(1)
+        keep = t >= 0
+        weight = keep * up.double() / (max(1, int(keep.sum())) if reduction == "mean" else 1)
+        p = torch.softmax(z, 1)
+        off = (weight.abs()[:, None] * p * (2 * row_off + 2.0 ** -16)[:, None]).sum(0)
+        p.scatter_add_(1, t.clamp_min(0)[:, None], -torch.ones_like(p[:, :1]))
+        p *= weight[:, None]
+        close(got, p.sum(0), off + 2.0 ** -19 * p.abs().sum(0) + 2.0 ** -23 * p.sum(0).abs(), size)
