@@ -27,7 +27,7 @@ namespace {
 
 struct Rows {
     Classes c;
-    int32_t n, v, tiles, reduction;
+    int32_t n, v, tiles;
     float *loss_row;       // reduction 0: the rows' losses
     double *sum;           // per block: sum and count
     double *count;
@@ -223,7 +223,6 @@ hipError_t loss_launch(const Loss &l, const void *x, int64_t ldx, const void *w,
         r.n = l.n;
         r.v = l.v;
         r.tiles = (int32_t)tiles;
-        r.reduction = l.reduction;
         r.loss_row = l.reduction == 0 ? loss : nullptr;
         r.sum = l.reduction == 0 ? nullptr : sum;
         r.count = cnt;
