@@ -513,6 +513,9 @@ rsc_status_t rsc_greedy_allocate_profiles(int32_t L, int32_t n, int64_t nnz, int
  *     be read) and, in outputs, not written.
  *   - Vectors (bias, its gradient) are contiguous, of the operands' type or,
  *     with bias_dtype RSC_F32, fp32.
+ *   - No output shares a value's place with an operand or another output
+ *     (RSC_ERR_INVALID_ARGUMENT), but where it says so. Column ranges of one
+ *     matrix are apart.
  *   - Workspaces are 256-byte aligned and private to the call until it
  *     completes on `stream`. All calls only launch kernels: they can be
  *     captured into a HIP graph, whose replays read and write the same
@@ -542,8 +545,7 @@ typedef struct {
 } rsc_linear_t;
 
 /* rsc_linear: bias, R and pre may be NULL; pre (n x m, fp32) receives Z, which
- * the backward pass of GELU and SiLU needs. Y may be R (in place) but must not
- * overlap X or W. fp32 products are formed from three bf16 parts a value
+ * the backward pass of GELU and SiLU needs. Y may be R (in place, ldy = ldr). fp32 products are formed from three bf16 parts a value
  * (24 bits in all, six partial products): finite operands of magnitude below
  * 3.3e38 give fp32 accuracy; an infinite operand gives NaN.
  * Workspace: 0 bytes unless the sums over k are split over blocks. */

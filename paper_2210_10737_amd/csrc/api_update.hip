@@ -58,6 +58,45 @@ rsc_status_t check_sizes(int32_t n, int32_t k, int32_t m, const char *what) {
     return check_tiles(m, k, what);
 }
 
+// An operand or result in memory: rows of `cols` bytes, `pitch` bytes apart.
+struct Area {
+    const void *p;
+    int64_t rows, cols, pitch;
+    const char *name;
+};
+Area area(const void *p, int64_t rows, int64_t cols, int64_t ld, size_t size, const char *name) {
+    return Area{p, rows, cols * (int64_t)size, ld * (int64_t)size, name};
+}
+Area line(const void *p, int64_t count, size_t size, const char *name) { return area(p, 1, count, count, size, name); }
+
+// Do they share a byte? Rows of the same pitch may lie in each other's gaps
+// (column ranges of one matrix); where pitches differ, ranges that meet count.
+bool meet(Area a, Area b) {
+    if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.cols <= 0 || b.cols <= 0) return false;
+    const int64_t from_a = (int64_t)(uintptr_t)a.p, from_b = (int64_t)(uintptr_t)b.p;
+    if (from_a + (a.rows - 1) * a.pitch + a.cols <= from_b || from_b + (b.rows - 1) * b.pitch + b.cols <= from_a)
+        return false;
+    if (a.rows == 1) a.pitch = b.pitch;
+    if (b.rows == 1) b.pitch = a.pitch;
+    if (a.pitch != b.pitch || (a.rows == 1 && b.rows == 1) || a.cols > a.pitch || b.cols > b.pitch) return true;
+    const int64_t at = ((from_b - from_a) % a.pitch + a.pitch) % a.pitch;  // of b's rows in a's
+    return at < a.cols || at + b.cols > a.pitch;
+}
+
+// No result lies on an operand or on another result.
+template <int O, int I>
+rsc_status_t check_apart(const Area (&outs)[O], const Area (&ins)[I], const char *what) {
+    for (int i = 0; i < O; ++i) {
+        for (int j = i + 1; j < O; ++j)
+            if (meet(outs[i], outs[j]))
+                return fail(RSC_ERR_INVALID_ARGUMENT, "%s: %s overlaps %s", what, outs[i].name, outs[j].name);
+        for (const Area &in : ins)
+            if (meet(outs[i], in))
+                return fail(RSC_ERR_INVALID_ARGUMENT, "%s: %s overlaps %s", what, outs[i].name, in.name);
+    }
+    return RSC_OK;
+}
+
 rsc_status_t check_linear(const rsc_linear_t *p) {
     if (!p) return fail(RSC_ERR_INVALID_ARGUMENT, "the layer is NULL");
     RSC_TRY(check_dtype(p->dtype, "dtype"));
@@ -91,6 +130,11 @@ rsc_status_t check_xent_operands(const rsc_xent_t *p, const void *X, int64_t ldx
     if (p->n > 0 && !targets) return fail(RSC_ERR_INVALID_ARGUMENT, "targets is NULL");
     if (!aligned(targets, p->targets_i32 ? 4 : 8)) return fail(RSC_ERR_UNSUPPORTED, "targets is misaligned");
     return RSC_OK;
+}
+
+Area xent_weights(const rsc_xent_t *p, const void *W, int64_t ldw) {
+    const size_t size = rsc::value_size(p->dtype);
+    return p->w_out_major ? area(W, p->v, p->k, ldw, size, "W") : area(W, p->k, p->v, ldw, size, "W");
 }
 
 rsc_status_t check_kept(const rsc_xent_t *p, const void *G, int64_t ldg) {
@@ -148,10 +192,16 @@ rsc_status_t rsc_linear(const rsc_linear_t *p, const void *X, int64_t ldx, const
     if (R) RSC_TRY(check_matrix(R, p->n, p->m, ldr, p->dtype, "R"));
     RSC_TRY(check_matrix(Y, p->n, p->m, ldy, p->dtype, "Y"));
     if (pre) RSC_TRY(check_matrix(pre, p->n, p->m, ldpre, RSC_F32, "pre"));
-    if (p->n > 0 && (Y == X || Y == W || (pre && (pre == Y || pre == X || pre == W))))
-        return fail(RSC_ERR_INVALID_ARGUMENT, "an output of the layer is one of its operands");
     if (p->n == 0) return RSC_OK;
     RSC_TRY(check_ws(ws, ws_bytes, rsc_linear_workspace_bytes(p), "linear"));
+    const size_t size = rsc::value_size(p->dtype);
+    const bool in_place = R == Y && (ldr == ldy || p->n == 1);
+    const Area outs[] = {area(Y, p->n, p->m, ldy, size, "Y"), area(pre, p->n, p->m, ldpre, 4, "pre")};
+    const Area ins[] = {area(X, p->n, p->k, ldx, size, "X"),
+                        p->w_out_major ? area(W, p->m, p->k, ldw, size, "W") : area(W, p->k, p->m, ldw, size, "W"),
+                        line(bias, p->m, rsc::value_size(bias_dtype), "bias"),
+                        area(in_place ? nullptr : R, p->n, p->m, ldr, size, "R")};
+    RSC_TRY(check_apart(outs, ins, "linear"));
     RSC_TRY(check_device());
     RSC_HIP(rsc::linear_launch(layer_of(p), X, ldx, W, ldw, bias, bias_dtype == RSC_F32, R, ldr, Y, ldy, pre, ldpre,
                                ws, stream),
@@ -186,6 +236,15 @@ rsc_status_t rsc_linear_backward(const rsc_linear_t *p, const void *dY, int64_t 
     RSC_TRY(check_ws(ws, ws_bytes, rsc_linear_backward_workspace_bytes(p, dX != nullptr, dW != nullptr,
                                                                        dbias != nullptr),
                      "linear backward"));
+    const size_t size = rsc::value_size(p->dtype);
+    const Area outs[] = {area(dX, p->n, p->k, lddx, size, "dX"), area(dW, w_rows, w_cols, lddw, size, "dW"),
+                         line(dbias, p->m, rsc::value_size(bias_dtype), "dbias"), area(dR, p->n, p->m, lddr, size, "dR")};
+    const Area ins[] = {area(dY, p->n, p->m, lddy, size, "dY"),
+                        area(p->act != RSC_ACT_NONE ? saved : nullptr, p->n, p->m, ldsaved,
+                             p->act == RSC_ACT_RELU ? size : 4, "saved"),
+                        area(dW ? X : nullptr, p->n, p->k, ldx, size, "X"),
+                        area(dX ? W : nullptr, w_rows, w_cols, ldw, size, "W")};
+    RSC_TRY(check_apart(outs, ins, "linear backward"));
     RSC_TRY(check_device());
     rsc::LinearGrads g;
     g.dx = dX;
@@ -216,6 +275,13 @@ rsc_status_t rsc_xent(const rsc_xent_t *p, const void *X, int64_t ldx, const voi
     if (p->reduction != 0) RSC_TRY(check_scalar(count, "count"));
     if (G) RSC_TRY(check_kept(p, G, ldg));
     RSC_TRY(check_ws(ws, ws_bytes, rsc_xent_workspace_bytes(p), "xent"));
+    const size_t size = rsc::value_size(p->dtype);
+    const Area outs[] = {line(loss, p->reduction == 0 ? p->n : 1, 4, "loss"), line(lse, p->n, 4, "lse"),
+                         line(p->reduction == 0 ? nullptr : count, 1, 4, "count"), area(G, p->n, p->v, ldg, size, "G")};
+    const Area ins[] = {area(X, p->n, p->k, ldx, size, "X"), xent_weights(p, W, ldw),
+                        line(bias, p->v, rsc::value_size(p->bias_dtype), "bias"),
+                        line(targets, p->n, p->targets_i32 ? 4 : 8, "targets")};
+    RSC_TRY(check_apart(outs, ins, "xent"));
     RSC_TRY(check_device());
     rsc::Classes c = classes_of(p, bias, targets);
     c.grad = G;
@@ -246,6 +312,17 @@ rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const vo
     RSC_TRY(check_ws(ws, ws_bytes,
                      rsc_xent_backward_workspace_bytes(p, dX != nullptr, dW != nullptr, G != nullptr),
                      "xent backward"));
+    const size_t size = rsc::value_size(p->dtype);
+    Area w_grad = xent_weights(p, dW, lddw);
+    w_grad.name = "dW";
+    const Area outs[] = {area(dX, p->n, p->k, lddx, size, "dX"), w_grad,
+                         line(dbias, p->v, rsc::value_size(p->bias_dtype), "dbias")};
+    const Area ins[] = {area(X, p->n, p->k, ldx, size, "X"), xent_weights(p, W, ldw),
+                        line(bias, p->v, rsc::value_size(p->bias_dtype), "bias"),
+                        line(targets, p->n, p->targets_i32 ? 4 : 8, "targets"),
+                        line(dloss, p->reduction == 0 ? p->n : 1, 4, "dloss"), line(lse, p->n, 4, "lse"),
+                        line(p->reduction == 0 ? nullptr : count, 1, 4, "count"), area(G, p->n, p->v, ldg, size, "G")};
+    RSC_TRY(check_apart(outs, ins, "xent backward"));
     RSC_TRY(check_device());
     rsc::LossGrads g;
     g.dx = dX;

@@ -168,3 +168,51 @@ def test_python_checks_without_a_device():
     with pytest.raises(ValueError):
         rsc.AdamW([torch.nn.Parameter(x)], state_bits=4)
     assert os.path.exists(rsc.LIB_PATH)
+
+
+def test_results_on_operands_are_refused():
+    """Also where only their ends, or some of their columns, meet."""
+    # X: 10 x 20 in rows of 32 (1,280 bytes), W: 20 x 12, ldw 32 (2,480 up to the last value)
+    assert forward(Y=0x1000 + 9 * 128 + 64) == BAD            # Y's first row in X's last one
+    assert forward(Y=0x2000 - 64 * 9 - 32, ldy=16) == BAD     # Y's last row in W's first one
+    assert forward(R=0x4040) == BAD                           # R a row further on than Y
+    assert forward(R=0x4000, ldr=32) == BAD                   # R is Y, in other rows
+    assert forward(bias=0x4000 + 64 * 4 + 16) == BAD
+    assert forward(pre=0x4000 + 64 * 3) == BAD
+    assert forward(X=0x1000, ldx=32, Y=0x1000 + 64, ldy=32) == BAD    # columns 16 to 27 of X's rows, X has 20
+
+    def back(p=None, dY=0x1000, X=0x2000, W=0x3000, dX=0x5000, lddx=32, dW=0x6000, db=None, dR=None, saved=None):
+        p = layer(act=1) if saved else layer()
+        return name(rsc.lib().rsc_linear_backward(ctypes.byref(p), dY, 16, saved, 16, X, 32, W, 16, dX, lddx, dW, 16, db, 0,
+                                                  dR, 16, WS, 1 << 30, None))
+
+    for bad in (dict(dX=0x1000), dict(dX=0x2000), dict(dX=0x3000), dict(dW=0x3000), dict(dW=0x2000 + 128), dict(dW=0x5000),
+                dict(dR=0x1000), dict(dR=0x6000), dict(db=0x3000), dict(db=0x5010), dict(saved=0x7000, dR=0x7000),
+                dict(saved=0x7000, dX=0x7000)):
+        assert back(**bad) == BAD, bad
+
+    def xent(out=0x4000, lse=0x5000, count=0x6000, G=None, X=0x1000, t=0x3000):
+        return name(rsc.lib().rsc_xent(ctypes.byref(loss()), X, 32, 0x2000, 16, None, t, out, lse, count, G, 16, WS, 1 << 30,
+                                       None))
+
+    for bad in (dict(out=0x5004), dict(lse=0x5000, count=0x5024), dict(lse=0x3010), dict(G=0x1000), dict(G=0x2000),
+                dict(out=0x1000), dict(G=0x8000, count=0x8000)):
+        assert xent(**bad) == BAD, bad
+
+    def xback(dX=0xa000, dW=0xb000, db=None, G=None):
+        return name(rsc.lib().rsc_xent_backward(ctypes.byref(loss()), 0x9000, 0x1000, 32, 0x2000, 16, None, 0x3000, 0x5000,
+                                                0x6000, G, 16, dX, 32, dW, 16, db, WS, 1 << 30, None))
+
+    for bad in (dict(dX=0x1000), dict(dW=0x2000), dict(dX=0x2000), dict(dX=0xb000), dict(db=0xa000), dict(db=0x5000),
+                dict(G=0x8000, dX=0x8010)):
+        assert xback(**bad) == BAD, bad
+
+
+@no_gpu
+def test_column_ranges_of_one_matrix_are_apart():
+    ok = "RSC_ERR_NO_DEVICE"
+    assert forward(X=0x10000, ldx=32, Y=0x10000 + 80, ldy=32) == ok       # columns 20 to 31 beside X's 0 to 19
+    assert forward(X=0x10000 + 48, ldx=32, Y=0x10000, ldy=32) == ok       # and before them
+    assert forward(R=0x4000) == ok                                        # in place
+    assert forward(layer(n=1), R=0x4000, ldr=32) == ok
+    assert forward(Y=0x1000 + 9 * 128 + 80) == ok                         # right behind X's last value
