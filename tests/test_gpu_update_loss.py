@@ -323,3 +323,38 @@ def test_an_fp32_bias_gets_its_gradient_from_unrounded_values(size, reduction, d
         p.scatter_add_(1, t.clamp_min(0)[:, None], -torch.ones_like(p[:, :1]))
         p *= weight[:, None]
         close(got, p.sum(0), off + 2.0 ** -19 * p.abs().sum(0) + 2.0 ** -23 * p.sum(0).abs(), size)
+
+
+@pytest.mark.parametrize("out_major", [False, True])
+@pytest.mark.parametrize("size", [(70, 8, 300), (150, 8, 41), (300, 5, 64), (513, 8, 1500), (1, 8, 5000), (2, 4, 70001)])
+def test_fp32_losses_to_the_accuracy_of_fp32(size, out_major):
+    """Short sums of k, so that the softmax's own error shows. In units of 2^-24:
+    arguments up to 32 rounded once (32), the sum's chain of up to 64 additions
+    in a lane, 4 waves and 16 joins with an exponential each, 8 tiles a thread with
+    two (100 additions, 40 exponentials of 4): below 2^-15 of a row's loss, and of
+    a probability with twice the logits' own error."""
+    n, k, v = size
+    x, w, b, t = inputs(n, k, v, torch.float32, out_major, 0.8, 41)
+    leaves = [a.requires_grad_() for a in (x, w, b)]
+    up = torch.full((), 1.5, device="cuda")
+    rows = rsc.linear_cross_entropy(x, w, t, b, reduction="none")
+    loss = rsc.linear_cross_entropy(x, w, t, b)
+    x6, w6 = x.detach().double(), w.detach().double()
+    z, mag = x6 @ w6 + b.detach().double(), x6.abs() @ w6.abs() + b.detach().double().abs()
+    assert float((z.amax(1) - z.amin(1)).max()) <= 32
+    row_off = (sums(k) * mag).amax(1)
+    keep, at = t >= 0, t.clamp_min(0)[:, None]
+    want = torch.where(keep, torch.logsumexp(z, 1) - z.gather(1, at)[:, 0], 0.0)
+    bound = 2 * row_off + 2.0 ** -15 + 2.0 ** -23 * want.abs()
+    close(rows.detach(), want, bound, "rows")
+    count = max(1, int(keep.sum()))
+    close(loss.detach(), want.sum() / count, (bound * keep).sum() / count + 2.0 ** -23 * want.sum() / count, "loss")
+    weight = (keep * 1.5 / count)[:, None]
+    p = torch.softmax(z, 1)
+    off = weight * p * (2 * row_off + 2.0 ** -15)[:, None]
+    p = weight * p.scatter_add(1, at, -torch.ones_like(p[:, :1]))
+    off = off + 2.0 ** -22 * p.abs()      # the differences and factors, held in fp32
+    gx, gw, gb = torch.autograd.grad(loss, leaves, up)
+    close(gx, p @ w6.t(), off @ w6.abs().t() + (sums(v) + 2.0 ** -22) * (p.abs() @ w6.abs().t()), "dx")
+    close(gw, x6.t() @ p, x6.abs().t() @ off + (sums(n) + 2.0 ** -22) * (x6.abs().t() @ p.abs()), "dw")
+    close(gb, p.sum(0), off.sum(0) + 2.0 ** -22 * p.abs().sum(0), "db")
