@@ -547,7 +547,8 @@ typedef struct {
 /* rsc_linear: bias, R and pre may be NULL; pre (n x m, fp32) receives Z, which
  * the backward pass of GELU and SiLU needs. Y may be R (in place, ldy = ldr). fp32 products are formed from three bf16 parts a value
  * (24 bits in all, six partial products): finite operands of magnitude below
- * 3.3e38 give fp32 accuracy; an infinite operand gives NaN.
+ * 3.3e38 give fp32 accuracy; an infinite operand gives NaN (one or two rows
+ * with w_out_major are multiplied as they are).
  * Workspace: 0 bytes unless the sums over k are split over blocks. */
 size_t rsc_linear_workspace_bytes(const rsc_linear_t *p);
 rsc_status_t rsc_linear(const rsc_linear_t *p, const void *X, int64_t ldx, const void *W, int64_t ldw,
@@ -609,7 +610,8 @@ rsc_status_t rsc_xent(const rsc_xent_t *p, const void *X, int64_t ldx, const voi
  * there for the same arguments, or NULL: the logits are then formed again. The
  * workspace holds one piece of the logits' gradient (256 MiB, or n x 2,048
  * values where that is more; none with G) and, with more than one piece, dX in
- * fp32. */
+ * fp32. fp16 with reduction 0: the rows share one scale, by which a row whose
+ * dloss is below 2^-24 of the largest loses bits of its gradients. */
 size_t rsc_xent_backward_workspace_bytes(const rsc_xent_t *p, int32_t with_dx, int32_t with_dw, int32_t with_g);
 rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const void *X, int64_t ldx, const void *W,
                                int64_t ldw, const void *bias, const void *targets, const float *lse,

@@ -26,8 +26,8 @@ Typical use (A_hat symmetric, so it serves as its own transpose):
 The update phase between two aggregations (fp32, bf16, fp16; differentiable):
 
     H = linear(P, W, b, residual=H, act="relu")          # act(P W + b + H)
-    loss = linear_cross_entropy(H, W_out, classes)       # no n x classes logits in memory
-    opt = AdamW(params, state_bits=8)                    # one launch over all tensors
+    loss = linear_cross_entropy(H, W_out, classes)       # logits in tiles, their gradient in pieces
+    opt = AdamW(params, state_bits=8)                    # a launch for each 44 tensors
 
 `gcn.GCNClassifier` is built from these and the aggregation.
 """

@@ -12,8 +12,8 @@
 // above zero keeps a code of at least 1, which bounds m / sqrt(v).
 //
 // Bound by memory (400M fp32 parameters with 8 bits 1.55 ms, 4.1 TB/s; 381M bf16
-// ones with masters 2.09 ms, 5.4 TB/s, parts of them in the caches) and, for small steps, by
-// the launch: every value is read and written once, 256 threads take
+// ones with masters, 28 bytes each, 2.09 ms, 5.1 TB/s, parts of them in the caches) and, for
+// small steps, by the launch: every value is read and written once, 256 threads take
 // 4,096 consecutive elements of a tensor, a wave 256 at a time (one block of
 // codes: its largest value is a reduction over the wave). All tensors of a
 // launch are in its arguments, so that a captured launch holds them.

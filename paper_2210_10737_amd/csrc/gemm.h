@@ -1063,7 +1063,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(Product p, Epilogue e) {
 // row the largest and the sum of exp(logit - largest): the logits stay in
 // registers. The lane that holds a row's own class writes its logit. Bound by the
 // matrix instructions where k is long (8192 x 4096 x 131,072 bf16: 7.6 ms, 1,160
-// TFLOP/s), by a tile's fixed part where it is short: 3001 x 1000 x 50,021 fp16 395 us,
+// TFLOP/s), by a tile's fixed part where it is short: 3001 x 1000 x 50,021 fp16 399 us,
 // 456 with a test and a select for each logit's bias and class.
 template <typename T, bool BC, typename C>
 __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes c) {
@@ -1195,8 +1195,9 @@ __global__ __launch_bounds__(C::THREADS, 1) void stats_kernel(Product p, Classes
 
 // The logits' gradient over one piece of the classes, from recomputed logits:
 // g = weight (exp(logit - lse) - [own class]) c.scale, zero for rows left out.
-// Bound as the statistics are: 3001 x 1000 x 25,088 fp16 219 us, 252 with the rows'
-// values read behind each store.
+// Bound as the statistics are: 3001 x 1000 x 25,088 fp16 227 us with the columns'
+// sums (222 without them; a pass over G takes 32), 252 with the rows' values read
+// behind each store.
 template <typename T, bool BC, typename C>
 __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes c) {
     using G = Tile<T, false, BC, C>;

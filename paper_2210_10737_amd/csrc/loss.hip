@@ -1,5 +1,5 @@
 // Softmax cross entropy of the logits X W + bias against one class a row, and
-// its gradients, without the logits in memory.
+// its gradients, with the logits in tiles.
 //
 // Forward: one product whose epilogue keeps, for each row and tile of classes,
 // the largest logit and the sum of exp(logit - largest); the tiles are joined

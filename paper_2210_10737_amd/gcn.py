@@ -27,7 +27,7 @@ device by rsc_cache_staleness from rsc_greedy_profile's ranking.
 GCN's dense update phase (MatMul, ReLU, loss, optimizer) uses torch; it is
 not part of the aggregation path. GCNClassifier's runs on the library: layer
 products with bias, residual and ReLU in their epilogue, softmax cross entropy
-without the logits in memory, and (with rsc.AdamW) the optimizer step.
+with its logits in tiles, and (with rsc.AdamW) the optimizer step.
 """
 from __future__ import annotations
 
@@ -267,7 +267,8 @@ class GCNClassifier(torch.nn.Module):
 
     Each layer aggregates first, so that bias, residual and ReLU are the
     epilogue of its product, every aggregation is `hidden` wide however many
-    classes there are, and the n x classes logits are never in memory."""
+    classes there are, and the n x classes logits are not stored (up to 64 classes
+    their gradient is, from the forward to the backward pass)."""
 
     def __init__(self, A: DeviceCsr, in_features: int, hidden: int, classes: int, cfg: RscConfig, layers: int = 2,
                  seed: int = 2, AT: DeviceCsr | None = None):

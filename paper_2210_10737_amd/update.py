@@ -294,14 +294,21 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.T
                          bias: torch.Tensor | None = None, ignore_index: int = -100,
                          reduction: str = "mean") -> torch.Tensor:
     """Softmax cross entropy (float32) of the logits x @ weight + bias against
-    one class a row, without the logits in memory (rsc_xent).
+    one class a row, without the logits in memory (rsc_xent): they are formed in
+    tiles, and their gradient in pieces of the classes.
 
     x [n, k], weight [k, v] in either storage order, bias [v] as in `linear`;
     targets int64 or int32 [n]. Rows of ignore_index count for nothing; any
     other target outside 0 .. v-1 gives NaN. reduction: mean over the rows that
     count (0 if there is none), sum, or none (a loss per row). Differentiable
     once in x, weight and bias: the logits are then formed again, except that
-    up to 64 classes the forward pass keeps their gradient (n x v values)."""
+    up to 64 classes the forward pass keeps their gradient (n x v values; not for
+    16-bit operands with a float32 bias that requires gradients). The logits'
+    gradient is rounded to x's type before dX and dW are formed from it.
+
+    A bias of -inf or of the lowest finite value takes a class out; where it takes
+    all of them out, gradients mean nothing. float16 with reduction none: rows
+    whose upstream gradient is below 2^-24 of the largest lose bits of theirs."""
     if reduction not in _REDUCTIONS:
         raise ValueError(f"reduction {reduction!r}: none, sum or mean expected")
     if targets.dtype not in (torch.int64, torch.int32):
