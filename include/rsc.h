@@ -610,8 +610,8 @@ rsc_status_t rsc_xent(const rsc_xent_t *p, const void *X, int64_t ldx, const voi
  * there for the same arguments, or NULL: the logits are then formed again. The
  * workspace holds one piece of the logits' gradient (256 MiB, or n x 2,048
  * values where that is more; none with G) and, with more than one piece, dX in
- * fp32. fp16 with reduction 0: the rows share one scale, by which a row whose
- * dloss is below 2^-24 of the largest loses bits of its gradients. */
+ * fp32. fp16 with reduction 0: rows of dX are exact beside their own dloss; what
+ * rows add to dW is held beside the largest dloss, and below 2^-34 of it lost. */
 size_t rsc_xent_backward_workspace_bytes(const rsc_xent_t *p, int32_t with_dx, int32_t with_dw, int32_t with_g);
 rsc_status_t rsc_xent_backward(const rsc_xent_t *p, const float *dloss, const void *X, int64_t ldx, const void *W,
                                int64_t ldw, const void *bias, const void *targets, const float *lse,

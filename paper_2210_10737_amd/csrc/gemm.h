@@ -1209,24 +1209,26 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
     const int tid = threadIdx.x;
     // a row's class, factor and log-sum-exp, on their way while the logits are formed
     int64_t own_class = -1;
-    float weight = 0.f, lse = 0.f;
+    float weight = 0.f, lse = 0.f, rel = 1.f;
     if (tid < BM && o.m * BM + tid < p.m) {
         own_class = c.target(o.m * BM + tid);
         weight = c.weight[o.m * BM + tid];
         lse = c.lse[o.m * BM + tid];
+        if (c.row_scale) rel = c.row_scale[o.m * BM + tid] / *c.over;
     }
     v16f acc[G::TA][G::TB];
     G::product(acc, p, lds, o.m * BM, o.n * BN, 0, (p.k + G::BK - 1) / G::BK);
     struct Row {
         float weight, base;
-        int own;  // counted from the tile's first class
+        int own;    // counted from the tile's first class
+        float rel;  // of the row's scale to the columns' sums'
     };
     constexpr int SLABS = 32 * (G::TB * 32 + 4) * 4 * (C::THREADS / 64);
     static_assert(SLABS + BM * (int)sizeof(Row) <= G::LDS, "the waves' rows and theirs");
     Row *const rows = (Row *)(lds + SLABS);
     if (tid < BM) {
         const int64_t t = own_class - c.first - (int64_t)o.n * BN;
-        rows[tid] = Row{weight * c.scale, lse, own_class >= 0 && t >= 0 && t < BN ? (int)t : -1};
+        rows[tid] = Row{weight * c.scale, lse, own_class >= 0 && t >= 0 && t < BN ? (int)t : -1, rel};
     }
     __syncthreads();
     const Spot at = spot_of<G, W>(p, o.m * BM, o.n * BN);
@@ -1250,7 +1252,7 @@ __global__ __launch_bounds__(C::THREADS, 1) void grad_kernel(Product p, Classes 
         }
         if (c.sums) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) column[i] += (Sum)v[i];
+            for (int i = 0; i < W; ++i) column[i] += (Sum)(v[i] * row.rel);
         }
         store_row((T *)c.grad + (at.m * c.ldgrad + at.n) + down * c.ldgrad, at.count, v);
     });

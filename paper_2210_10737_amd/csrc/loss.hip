@@ -12,7 +12,12 @@
 //
 // G has no small factors in it (1/count, the upstream gradient): those go into
 // the products' fp32 epilogues. fp16's G is scaled by 2^10 as well, so that
-// probabilities down to 2^-34 are not lost.
+// probabilities down to 2^-34 are not lost. Gradients of single rows (reduction
+// "none") may differ by any factor, too: under the largest one's scale a row 2^24
+// times smaller would lose bits of its dX. So in fp16 each row is formed at a
+// scale of its own, dX at that scale, and dX's and, for dW, G's rows are then taken to
+// the common one by powers of two: exact, but for dX's own subnormal values, which
+// are rounded twice, and for rows of G that are nothing beside the others in dW.
 //
 // Up to 64 classes (n x 64 values beside the n x k of X) the forward pass can
 // leave G, since it has all of a row's logits in one tile: the backward pass then
@@ -145,15 +150,50 @@ __global__ __launch_bounds__(1024) void factor_kernel(Classes c, const float *dl
     }
 }
 
-// A row's weight: 0 for one that is left out, NaN for a class out of range
+// A row's weight: 0 for one that is left out, NaN for a class out of range.
+// row_scale (nullable): the row's own power of two, by which its weight is divided
+// to 1/4 .. 1/2 in magnitude in place of the factor (non-finite ones stay).
 __global__ __launch_bounds__(256) void weight_kernel(Classes c, const float *dloss, const float *factor, int32_t n,
-                                                     int32_t v, int32_t by_row, float *weight) {
+                                                     int32_t v, int32_t by_row, float *weight, float *row_scale) {
     const int m = blockIdx.x * 256 + threadIdx.x;
     if (m >= n) return;
     const int64_t t = c.targets_i32 ? (int64_t)((const int32_t *)c.targets)[m] : ((const int64_t *)c.targets)[m];
+    float by = by_row ? *factor : 1.f;
+    if (row_scale) {
+        const float up = fabsf(dloss[m]);
+        by = up > 0.f && up <= 3.4e38f ? ldexpf(4.f, max(-120, min(120, ilogbf(up)))) : 1.f;
+        row_scale[m] = by;
+    }
     float w = 0.f;
-    if (t != c.ignore) w = t >= 0 && t < v ? (by_row ? dloss[m] / *factor : 1.f) : NAN;
+    if (t != c.ignore) w = t >= 0 && t < v ? (by_row ? dloss[m] / by : 1.f) : NAN;
     weight[m] = w;
+}
+
+// Rows times powers of two: row_scale[m], over *over if that is given
+__global__ __launch_bounds__(256) void scale_rows_kernel(_Float16 *p, int64_t ld, int32_t rows, int32_t cols,
+                                                         const float *row_scale, const float *over) {
+    const int64_t chunks = (cols + 7) / 8, step = (int64_t)gridDim.x * 256;
+    typedef _Float16 vec __attribute__((ext_vector_type(8)));
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks * rows; i += step) {
+        const int64_t m = i / chunks;
+        const int c = (int)(i % chunks) * 8;
+        const float by = over ? row_scale[m] / *over : row_scale[m];
+        _Float16 *const at = p + m * ld + c;
+        if (cols - c >= 8) {
+            vec x = *(const vec *)at;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = (_Float16)((float)x[j] * by);
+            *(vec *)at = x;
+        } else {
+            for (int j = 0; j < cols - c; ++j) at[j] = (_Float16)((float)at[j] * by);
+        }
+    }
+}
+hipError_t scale_rows(void *p, int64_t ld, int32_t rows, int32_t cols, const float *row_scale, const float *over,
+                      hipStream_t stream) {
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div((int64_t)rows * ((cols + 7) / 8), 256), 8192);
+    scale_rows_kernel<<<grid, 256, 0, stream>>>((_Float16 *)p, ld, rows, cols, row_scale, over);
+    return hipGetLastError();
 }
 
 constexpr size_t kPieceBytes = size_t(256) << 20;
@@ -259,6 +299,8 @@ size_t sums_bytes(const Loss &l, bool kept) {
         if (v > 0) b = std::max(b, sizeof(double) * (size_t)(v * ceil_div(l.n, kShapes[loss_shape(l.dtype, l.n, v, l.k)].bm)));
     return align_up(b, 256);
 }
+// do rows have scales of their own?
+bool own_scales(const Loss &l, bool dx) { return dx && l.dtype == kF16 && l.reduction == 0; }
 int64_t grad_ld(const Loss &l) { return (int64_t)align_up((size_t)piece_of(l), 16 / value_size(l.dtype)); }
 int64_t acc_ld(const Loss &l) { return (int64_t)align_up((size_t)l.k, 4); }
 }  // namespace
@@ -269,6 +311,7 @@ size_t loss_backward_ws_bytes(const Loss &l, bool dx, bool dw, bool kept) {
     if (!kept)
         b += align_up((size_t)l.n * grad_ld(l) * value_size(l.dtype), 256) + align_up(sizeof(float) * (size_t)l.n, 256);
     if (dx && piece_of(l) < l.v) b += align_up(sizeof(float) * (size_t)l.n * acc_ld(l), 256);
+    if (own_scales(l, dx)) b += align_up(sizeof(float) * (size_t)l.n, 256);
     return b;
 }
 
@@ -301,14 +344,21 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
         acc = (float *)at;
         at += align_up(sizeof(float) * (size_t)l.n * acc_ld(l), 256);
     }
+    float *row_scale = nullptr;
+    if (own_scales(l, g.dx != nullptr)) {
+        row_scale = (float *)at;
+        at += align_up(sizeof(float) * (size_t)l.n, 256);
+    }
     void *cut = at;
     factor_kernel<<<1, 1024, 0, stream>>>(c, dloss, count, l.n, l.reduction == 0, factor);
     if (!kept)
         weight_kernel<<<(unsigned)ceil_div(l.n, 256), 256, 0, stream>>>(c, dloss, factor, l.n, l.v, l.reduction == 0,
-                                                                        weight);
+                                                                        weight, row_scale);
     e = hipGetLastError();
     c.weight = weight;
-    c.scale = grad_scale(l);
+    c.scale = grad_scale(l) * (row_scale ? 4.f : 1.f);
+    c.row_scale = row_scale;
+    c.over = factor;
     c.sums = g.db && !kept ? (double *)sums : nullptr;
     const void *bias = c.bias;
     for (int64_t v0 = 0; v0 < l.v && e == hipSuccess; v0 += piece) {
@@ -338,7 +388,7 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
             const bool last = v0 + vc >= l.v;
             Epilogue o;
             o.alpha = 1.f / c.scale;
-            o.alpha_dev = factor;
+            o.alpha_dev = row_scale ? nullptr : factor;
             if (v0 > 0) {
                 o.r = acc;
                 o.ldr = acc_ld(l);
@@ -348,7 +398,9 @@ hipError_t loss_backward_launch(const Loss &l, const float *dloss, const void *x
             o.ldy = last ? g.lddx : acc_ld(l);
             o.y_f32 = last ? 0 : 1;
             e = product_launch(l.dtype, l.out_major ? kRowsCols : kRowsRows, q, o, cut, stream);
+            if (row_scale && last && e == hipSuccess) e = scale_rows(g.dx, g.lddx, l.n, l.k, row_scale, nullptr, stream);
         }
+        if (row_scale && g.dw && e == hipSuccess) e = scale_rows(c.grad, c.ldgrad, l.n, vc, row_scale, factor, stream);
         if (g.dw && e == hipSuccess) {
             Product q;
             q.a = l.out_major ? c.grad : x;

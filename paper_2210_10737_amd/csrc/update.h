@@ -62,6 +62,9 @@ struct Classes {
     int64_t first = 0;  // the piece's first class
     void *grad = nullptr;
     int64_t ldgrad = 0;
+    // fp16, nullable: what the rows' weights are divided by, and the factor that the
+    // columns' sums are under
+    const float *row_scale = nullptr, *over = nullptr;
     double *sums = nullptr;  // gradient pass, nullable: each row of tiles' column sums, the piece's width apart
 
     __device__ __forceinline__ int64_t raw(int m) const {

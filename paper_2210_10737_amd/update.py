@@ -307,8 +307,9 @@ def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.T
     gradient is rounded to x's type before dX and dW are formed from it.
 
     A bias of -inf or of the lowest finite value takes a class out; where it takes
-    all of them out, gradients mean nothing. float16 with reduction none: rows
-    whose upstream gradient is below 2^-24 of the largest lose bits of theirs."""
+    all of them out, gradients mean nothing. float16 with reduction none: dX's
+    rows are held beside their own upstream gradient, what they add to dW beside the
+    largest one (below 2^-34 of it, it is lost)."""
     if reduction not in _REDUCTIONS:
         raise ValueError(f"reduction {reduction!r}: none, sum or mean expected")
     if targets.dtype not in (torch.int64, torch.int32):

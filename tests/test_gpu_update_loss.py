@@ -358,3 +358,49 @@ def test_fp32_losses_to_the_accuracy_of_fp32(size, out_major):
     close(gx, p @ w6.t(), off @ w6.abs().t() + (sums(v) + 2.0 ** -22) * (p.abs() @ w6.abs().t()), "dx")
     close(gw, x6.t() @ p, x6.abs().t() @ off + (sums(n) + 2.0 ** -22) * (x6.abs().t() @ p.abs()), "dw")
     close(gb, p.sum(0), off.sum(0) + 2.0 ** -22 * p.abs().sum(0), "db")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(96, 48, 300), (64, 1000, 41), (66000, 16, 2300), (2, 64, 300)])
+def test_upstream_gradients_of_any_size_keep_their_rows(size, dtype):
+    """Reduction "none", the rows' upstream gradients from 2^12 down to 2^-10: each
+    row of dX is right beside its own upstream gradient, not only the largest."""
+    n, k, v = size
+    x, w, b, t = inputs(n, k, v, dtype, True, 0.9, 51)
+    for a in (x, w, b):
+        a.requires_grad_()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    up = torch.randn(n, generator=g, device="cuda") * 2.0 ** (12 - torch.arange(n, device="cuda") % 23)
+    up[0] = 2.0 ** 12
+    up[1] = 0.0
+    loss = rsc.linear_cross_entropy(x, w, t, b, reduction="none")
+    _, _, grad, grad_off, grad_mag, _ = reference(x, w, b, t, -100, "none", up)
+    got = torch.autograd.grad(loss, [x, w, b], up)
+    # fp16: half of the smallest step, 2^-25 over 2^10, beside the row's own upstream gradient
+    tiny = up.abs().double()[:, None] * 2.0 ** -34 if dtype == torch.float16 else 0.0
+    grad_off = grad_off + (half(dtype) * grad_mag + tiny * (grad_mag > 0)) * (1 if dtype != torch.float32 else 0.5) \
+        + 2.0 ** -22 * grad_mag
+    x6, w6 = x.detach().double(), w.detach().double()
+    small = torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps   # a result's own smallest step
+    want, mag = grad @ w6.t(), (grad_mag + grad_off) @ w6.abs().t()
+    off = grad_off @ w6.abs().t() + (sums(v) + 4 * 2.0 ** -23) * mag
+    close(got[0], want, off + half(dtype) * (want.abs() + off) + small, "dx")
+    assert not got[0][t == -100].any() and not got[0][1].any()
+    # in the sums over rows what is lost is beside the largest one
+    if dtype == torch.float16:
+        grad_off = grad_off + up.abs().max().double() * 2.0 ** -34 * (grad_mag > 0)
+    want, off = x6.t() @ grad, x6.abs().t() @ grad_off + (sums(n) + 2.0 ** -23) * (x6.abs().t() @ (grad_mag + grad_off))
+    close(got[1], want, off + half(dtype) * (want.abs() + off) + small, "dw")
+    want, off = grad.sum(0), grad_off.sum(0)
+    close(got[2], want, off + half(b.dtype) * (want.abs() + off) + small, "db")
+
+
+def test_fp16_upstream_gradients_that_are_not_finite_stay_in_their_rows():
+    x, w, b, t = inputs(40, 32, 300, torch.float16, True, 1.0, 52)
+    x.requires_grad_()
+    up = torch.full((40,), 8.0, device="cuda")
+    want, = torch.autograd.grad(rsc.linear_cross_entropy(x, w, t, b, reduction="none"), x, up)
+    up[3], up[7] = float("inf"), float("nan")
+    got, = torch.autograd.grad(rsc.linear_cross_entropy(x, w, t, b, reduction="none"), x, up)
+    rest = torch.tensor([i not in (3, 7) for i in range(40)], device="cuda")
+    assert torch.equal(got[rest], want[rest]) and not got[3].isfinite().any() and bool(got[7].isnan().all())
