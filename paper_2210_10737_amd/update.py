@@ -9,7 +9,8 @@ such rows, so chained calls copy nothing.
 `linear` and `linear_cross_entropy` are differentiable once. Everything runs
 on the current stream and can be captured into a HIP graph, a forward pass
 together with its backward pass: the backward pass of one that ran outside the
-capture cannot be captured.
+capture cannot be captured, nor, by torch's own rule, a `backward()` while a result
+of an eager pass over the same leaves is held (drop such losses before).
 """
 from __future__ import annotations
 

@@ -90,3 +90,46 @@ def test_refusals():
     for bad in (dict(hidden=30), dict(layers=0)):
         with pytest.raises(ValueError):
             setup(RscConfig(), **bad)
+
+
+@pytest.mark.parametrize("dtype,bits", [(torch.float32, 32), (torch.bfloat16, 8)])
+def test_a_whole_step_captured_is_the_eager_one(dtype, bits):
+    """Layer, loss, gradients and optimizer in one graph, replayed between eager
+    steps of a twin."""
+    def build():
+        g = torch.Generator(device="cuda").manual_seed(8)
+        ps = [torch.nn.Parameter((torch.randn(s, generator=g, device="cuda") / 8).to(dtype))
+              for s in ((50, 70), (70,), (70, 41), (41,))]
+        return ps, rsc.AdamW(ps, lr=1e-2, state_bits=bits)
+
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x, r = (torch.randn((200, c), generator=g, device="cuda").to(dtype) for c in (50, 70))
+    t = torch.randint(0, 41, (200,), generator=g, device="cuda")
+    t[::7] = -100
+
+    def step(ps, opt):
+        loss = rsc.linear_cross_entropy(rsc.linear(x, ps[0], ps[1], residual=r, act="relu"), ps[2], t, ps[3])
+        for p, d in zip(ps, torch.autograd.grad(loss, ps)):
+            p.grad = d
+        opt.step()
+        return loss.detach()
+
+    (ps, opt), (qs, twin) = build(), build()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step(ps, opt)
+    torch.cuda.current_stream().wait_stream(stream)
+    step(qs, twin)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss = step(ps, opt)
+    for i in range(4):
+        with torch.no_grad():
+            x.mul_(0.9)
+            t[i] = i
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(qs, twin)
+        assert torch.equal(loss, want) and all(torch.equal(p, q) for p, q in zip(ps, qs)), i
+    assert int(opt.param_groups[0]["step"]) == int(twin.param_groups[0]["step"]) == 5
