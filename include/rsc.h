@@ -533,8 +533,9 @@ typedef enum { RSC_ACT_NONE = 0, RSC_ACT_RELU = 1, RSC_ACT_GELU = 2, RSC_ACT_SIL
  *   act: none, max(z, 0), z Phi(z) (the exact GELU), z / (1 + exp(-z)).
  *   for_gradients: with ReLU, the sign of results next to zero, on which
  *   gradients hang, is decided by sums in 64 bits (at most 32 in each group of
- *   some thousand results; next to zero beside the largest result of the same
- *   row), and a positive one does not round to 0; without effect otherwise. */
+ *   some thousand results; next to zero beside the largest of the group or, in a
+ *   row of a scale far below, of the row), and a positive one does not round to 0;
+ *   without effect otherwise. */
 typedef struct {
     int32_t dtype; /* rsc_dtype_t of X, W, R, Y */
     int32_t act;   /* rsc_act_t */
@@ -545,9 +546,9 @@ typedef struct {
 } rsc_linear_t;
 
 /* rsc_linear: bias, R and pre may be NULL; pre (n x m, fp32) receives Z, which
- * the backward pass of GELU and SiLU needs. Y may be R (in place, ldy = ldr). fp32 products are formed from three bf16 parts a value
- * (24 bits in all, six partial products): finite operands of magnitude below
- * 3.3e38 give fp32 accuracy; an infinite operand gives NaN (one or two rows
+ * the backward pass of GELU and SiLU needs. Y may be R (in place, ldy = ldr).
+ * fp32 products are formed from three bf16 parts a value (24 bits in all, six
+ * partial products): finite operands of magnitude below 3.3e38 give fp32 accuracy; an infinite operand gives NaN (one or two rows
  * with w_out_major are multiplied as they are).
  * Workspace: 0 bytes unless the sums over k are split over blocks. */
 size_t rsc_linear_workspace_bytes(const rsc_linear_t *p);

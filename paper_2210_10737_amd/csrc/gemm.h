@@ -620,14 +620,20 @@ __device__ __forceinline__ double dot64(const Product &p, int b_cols, int m, int
     return sum;
 }
 
-// How far a sum of k terms may be off, from the largest sum of its row near by: a
-// random walk of roundings takes it 2^-24 sqrt(k / 16) of that, this is more
-// than ten times as far. By rows, since rows of A may differ by any factor: under
-// the largest sum of all, one row takes the whole list for its neighbours. From
-// fewer than kScaleOf columns a row's scale does not show (all of them may be next
-// to zero), and the wave's largest sum stands for it.
-constexpr int kScaleOf = 8;
+// How far a sum of k terms may be off, from the largest sum around it: a random
+// walk of roundings takes it 2^-24 sqrt(k / 16) of that, this is more than ten
+// times as far.
 __device__ __forceinline__ float doubt_of(float largest, int k) { return largest * 0x1p-24f * (8.f + sqrtf((float)k)); }
+
+// The largest sum around one of a row: the wave's, which sees the scale of every
+// column, unless the row's own is 2^10 times smaller, as beside a row of another
+// scale in A: then ordinary results would count as next to zero, too many of them
+// for the list (up to that factor some 16 of 8,192). From fewer than kScaleOf
+// columns a row's own scale does not show, since all of them may be next to zero.
+constexpr int kScaleOf = 8;
+__device__ __forceinline__ float largest_around(float row, float wave, int columns) {
+    return columns >= kScaleOf && row * 1024.f < wave ? row : wave;
+}
 
 // Is an argument next to zero? `others`: the magnitudes added to the sum. A sum
 // of exactly 0 is taken as such (a row of zeros).
@@ -831,11 +837,11 @@ __global__ __launch_bounds__(C::THREADS, 1) void product_kernel(Product p, Epilo
             largest[i] = fmaxf(largest[i], __shfl_xor(largest[i], 32));
             all = fmaxf(all, largest[i]);
         }
-        const bool few = p.n - (o.n * BN + (wave % C::WN) * G::TB * 32) < kScaleOf;
-        if (few) all = wave_max(all);
+        all = wave_max(all);
+        const int columns = p.n - (o.n * BN + (wave % C::WN) * G::TB * 32);
 #pragma unroll
         for (int i = 0; i < G::TA; ++i)
-            doubts[i * 32 + (lane & 31)] = doubt_of(fabsf(alpha) * (few ? all : largest[i]), p.k);
+            doubts[i * 32 + (lane & 31)] = doubt_of(fabsf(alpha) * largest_around(largest[i], all, columns), p.k);
     }
     with_act<AC>(e.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
@@ -954,8 +960,8 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, Epilogue e) {
             const int row = __shfl_down(m, d);
             if ((int)(threadIdx.x & 63) + d < 64 && row == m) largest = fmaxf(largest, above);
         }
-        const bool few = min(to_chunk * W, p.n) - from_chunk * W < kScaleOf;
-        const float doubt = doubt_of(fabsf(alpha) * (few ? all : largest), p.k);
+        const int columns = min(to_chunk * W, p.n) - from_chunk * W;
+        const float doubt = doubt_of(fabsf(alpha) * largest_around(largest, all, columns), p.k);
         // places: the value's number among the wave's
         again.note<T>(v, sum, bias, r, e, doubt, (threadIdx.x & 63) * W, live ? count : 0);
     }

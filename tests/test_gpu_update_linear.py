@@ -453,3 +453,23 @@ def test_results_can_be_changed_in_place(n, m, dtype):
     assert not g._is_view() and (g.stride(0) == 1 or m == 1)
     y = rsc.linear(x2, w2)      # (without gradients)
     y.mul_(2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(4992, 300, 320), (320, 300, 64), (5, 300, 640)])
+def test_relu_masks_of_columns_of_another_scale(size, dtype):
+    """One column in 64 is 2^8 times as large as the others, and its bias takes the
+    sum of one row away but its rounding: decided in 64 bits, though the row's
+    other results are small."""
+    n, k, m = size
+    g = torch.Generator(device="cuda").manual_seed(22)
+    x, w = rand((n, k), dtype, g), rand((k, m), dtype, g, 1 / math.sqrt(k))
+    w[:, 5::64] *= 2.0 ** 8
+    b = rand((m,), torch.float32, g)
+    exact = x.double() @ w.double()
+    column = torch.arange(5, m, 64, device="cuda")
+    for first in range(0, min(n, 96), 3):      # many rows, one after the other
+        row = (first + column) % n
+        b[column] = -exact[row, column].float()
+        y = rsc.linear(x.clone().requires_grad_(), w, b, act="relu").detach()
+        assert torch.equal(y > 0, exact + b.double() > 0), first
